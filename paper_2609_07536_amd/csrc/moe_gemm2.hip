@@ -43,6 +43,7 @@
 #include <unordered_map>
 
 #include "moe_gemm2.h"
+#include "status_bits.h"
 
 namespace {
 
@@ -73,8 +74,6 @@ constexpr int kYPad = 64;     // Y row padding, elements
 // now and then, when they ran on different XCDs.)
 constexpr int kYLine = 64;    // elements per 128-byte line
 __host__ __device__ inline int round_up_line(int n) { return (n + kYLine - 1) / kYLine * kYLine; }
-constexpr uint32_t kStBadRouting = 1u;
-constexpr uint32_t kStTimeout = 2u;
 
 typedef __bf16 bf16x8 __attribute__((__vector_size__(8 * sizeof(__bf16))));
 typedef float f32x4 __attribute__((ext_vector_type(4)));

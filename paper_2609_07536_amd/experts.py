@@ -1,0 +1,192 @@
+"""ctypes binding of the operators around and inside the experts
+(include/moe_experts.h): argument marshalling only, like ``binding``.
+
+Tensors are contiguous and on the GPU.  Every function takes ``stream`` (a
+torch stream; default: the current one) and only enqueues work on it; outputs
+that are not given with ``out`` are allocated for that stream.  ``workspace``
+(a ``binding.Workspace`` of at least 512 bytes) is where the row operators
+record bad entries of ``slot_rows`` or ``row_ids`` for ``Workspace.status``.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import NamedTuple, Optional
+
+import torch
+
+from .binding import MoeError, Workspace, _stream
+from .binding import lib as _base_lib
+
+EXPORTED = (
+    "moe_sort_scratch_size", "moe_sort_by_expert", "moe_dispatch_rows", "moe_dispatch_rows_grad",
+    "moe_combine_rows", "moe_combine_rows_grad", "moe_experts_abi_version",
+)
+
+_TYPES = {torch.bfloat16: 0, torch.float32: 1}   # moe_type_t
+_lib = None
+
+
+def lib() -> ctypes.CDLL:
+    """The HIP library with this module's functions declared."""
+    global _lib
+    if _lib is None:
+        L = _base_lib()
+        vp, sz, i32, i64 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32, ctypes.c_int64
+        L.moe_sort_scratch_size.argtypes = [i32, i32, i32]
+        L.moe_sort_scratch_size.restype = sz
+        L.moe_sort_by_expert.argtypes = [vp] * 6 + [i32] * 4 + [vp, sz, vp]
+        L.moe_dispatch_rows.argtypes = [vp] * 3 + [i32, i32, i64, i64, vp, vp]
+        L.moe_dispatch_rows_grad.argtypes = [vp] * 3 + [i32, i32, i64, i32, i32, i32, vp, vp]
+        L.moe_combine_rows.argtypes = [vp] * 4 + [i32, i32, i64, i32, i32, i32, vp, vp]
+        L.moe_combine_rows_grad.argtypes = [vp] * 6 + [i32, i32, i64, i32, i32, i32, vp, vp]
+        for name in EXPORTED:
+            if name != "moe_sort_scratch_size":
+                getattr(L, name).restype = ctypes.c_int
+        _lib = L
+    return _lib
+
+
+def _check(t, what, shape, *dtypes):
+    if t.dtype not in dtypes or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+        raise TypeError(f"{what}: expected a contiguous CUDA tensor of {' or '.join(map(str, dtypes))} and shape "
+                        f"{tuple(shape)}, got {t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
+
+
+def _empty(shape, dtype, device, stream):
+    """Memory for a launch on `stream`: the caching allocator hands it out again
+    only for later work on that stream."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _output(out, what, shape, device, stream, *dtypes):
+    if out is None:
+        return _empty(shape, dtypes[0], device, stream)
+    _check(out, what, shape, *dtypes)
+    return out
+
+
+def _two(t, what, *dtypes):
+    if t.dim() != 2:
+        raise TypeError(f"{what}: expected two dimensions, got {tuple(t.shape)}")
+    _check(t, what, t.shape, *dtypes)
+    return t.shape
+
+
+def _done(r, what):
+    if r < 0:
+        raise MoeError(r, what)
+
+
+def _status_word(workspace):
+    return workspace.ptr if workspace is not None else None
+
+
+class Routing(NamedTuple):
+    """A router's choice as rows grouped by expert, as the stage and the grouped
+    products take it: expert_offsets int32 [E + 1]; token_ids int32 and gate_w
+    fp32 [T topk], of which the first expert_offsets[E] are rows (then -1 and
+    0); slot_rows int32 [T, topk], the row of each of a token's slots or -1."""
+    expert_offsets: torch.Tensor
+    token_ids: torch.Tensor
+    gate_w: torch.Tensor
+    slot_rows: torch.Tensor
+
+
+def sort_by_expert(expert_ids, gates, E: int, first_expert: int = 0, out: Optional[Routing] = None,
+                   scratch=None, stream=None) -> Routing:
+    """moe_sort_by_expert: expert_ids int32 and gates fp32 [T, topk] to a Routing
+    (a stable sort by expert).  Ids outside [first_expert, first_expert + E)
+    are slots without a row.  scratch: uint8, at least sort_scratch_size bytes."""
+    T, topk = shape = _two(expert_ids, "expert_ids", torch.int32)
+    _check(gates, "gates", shape, torch.float32)
+    L, n, dev = lib(), T * topk, expert_ids.device
+    if out is None:
+        out = Routing(_empty((E + 1,), torch.int32, dev, stream), _empty((n,), torch.int32, dev, stream),
+                      _empty((n,), torch.float32, dev, stream), _empty(shape, torch.int32, dev, stream))
+    else:
+        _check(out.expert_offsets, "expert_offsets", (E + 1,), torch.int32)
+        _check(out.token_ids, "token_ids", (n,), torch.int32)
+        _check(out.gate_w, "gate_w", (n,), torch.float32)
+        _check(out.slot_rows, "slot_rows", shape, torch.int32)
+    need = L.moe_sort_scratch_size(T, topk, E) if n > 4096 else 0
+    if need and scratch is None:
+        scratch = _empty((need,), torch.uint8, dev, stream)
+    elif need:
+        _check(scratch, "scratch", scratch.shape, torch.uint8)
+    _done(L.moe_sort_by_expert(expert_ids.data_ptr(), gates.data_ptr(), out.expert_offsets.data_ptr(),
+                               out.token_ids.data_ptr(), out.gate_w.data_ptr(), out.slot_rows.data_ptr(),
+                               T, topk, E, first_expert, scratch.data_ptr() if need else None,
+                               scratch.numel() if need else 0, _stream(stream)), "moe_sort_by_expert")
+    return out
+
+
+def sort_scratch_size(T: int, topk: int, E: int) -> int:
+    return int(lib().moe_sort_scratch_size(T, topk, E))
+
+
+def dispatch_rows(x, slot_rows, rows: int, out=None, workspace: Optional[Workspace] = None, stream=None):
+    """moe_dispatch_rows: x [T, H] of any type to [rows, H], each token's row
+    copied to the rows of its slots.  Rows that no slot has are not written."""
+    T, topk = _two(slot_rows, "slot_rows", torch.int32)
+    _two(x, "x", x.dtype)
+    H = x.shape[1]
+    _check(x, "x", (T, H), x.dtype)
+    out = _output(out, "out", (rows, H), x.device, stream, x.dtype)
+    _done(lib().moe_dispatch_rows(x.data_ptr(), slot_rows.data_ptr(), out.data_ptr(), T, topk, rows,
+                                  H * x.element_size(), _status_word(workspace), _stream(stream)),
+          "moe_dispatch_rows")
+    return out
+
+
+def dispatch_rows_grad(d, slot_rows, out=None, workspace: Optional[Workspace] = None, stream=None):
+    """moe_dispatch_rows_grad: d [rows, H] (bf16 or fp32) to dx [T, H] (of d's type,
+    or `out`'s): the sum of each token's rows, in fp32, rounded once."""
+    T, topk = _two(slot_rows, "slot_rows", torch.int32)
+    rows, H = _two(d, "d", torch.bfloat16, torch.float32)
+    if out is None:
+        out = _empty((T, H), d.dtype, d.device, stream)
+    else:
+        _check(out, "out", (T, H), torch.bfloat16, torch.float32)
+    _done(lib().moe_dispatch_rows_grad(d.data_ptr(), slot_rows.data_ptr(), out.data_ptr(), T, topk, rows, H,
+                                       _TYPES[d.dtype], _TYPES[out.dtype], _status_word(workspace),
+                                       _stream(stream)), "moe_dispatch_rows_grad")
+    return out
+
+
+def combine_rows(y, slot_rows, gates, out=None, dtype=torch.float32, workspace: Optional[Workspace] = None,
+                 stream=None):
+    """moe_combine_rows: y [rows, H] (bf16 or fp32) to out [T, H] (`dtype`: fp32 or
+    bf16): the sum of each token's rows weighted by gates fp32 [T, topk], in
+    fp32, rounded once."""
+    T, topk = shape = _two(slot_rows, "slot_rows", torch.int32)
+    _check(gates, "gates", shape, torch.float32)
+    rows, H = _two(y, "y", torch.bfloat16, torch.float32)
+    if out is None:
+        out = _empty((T, H), dtype, y.device, stream)
+    _check(out, "out", (T, H), torch.bfloat16, torch.float32)
+    _done(lib().moe_combine_rows(y.data_ptr(), slot_rows.data_ptr(), gates.data_ptr(), out.data_ptr(), T, topk,
+                                 rows, H, _TYPES[y.dtype], _TYPES[out.dtype], _status_word(workspace),
+                                 _stream(stream)), "moe_combine_rows")
+    return out
+
+
+def combine_rows_grad(d_out, y, slot_rows, gates, out=None, workspace: Optional[Workspace] = None, stream=None):
+    """moe_combine_rows_grad: d_out [T, H] and y [rows, H] (each bf16 or fp32) to
+    (dy [rows, H] of y's type, dgates fp32 [T, topk]); `out`: that pair."""
+    T, topk = shape = _two(slot_rows, "slot_rows", torch.int32)
+    _check(gates, "gates", shape, torch.float32)
+    rows, H = _two(y, "y", torch.bfloat16, torch.float32)
+    _check(d_out, "d_out", (T, H), torch.bfloat16, torch.float32)
+    if out is None:
+        out = (_empty((rows, H), y.dtype, y.device, stream), _empty(shape, torch.float32, y.device, stream))
+    else:
+        _check(out[0], "dy", (rows, H), y.dtype)
+        _check(out[1], "dgates", shape, torch.float32)
+    _done(lib().moe_combine_rows_grad(d_out.data_ptr(), y.data_ptr(), slot_rows.data_ptr(), gates.data_ptr(),
+                                      out[0].data_ptr(), out[1].data_ptr(), T, topk, rows, H,
+                                      _TYPES[d_out.dtype], _TYPES[y.dtype], _status_word(workspace),
+                                      _stream(stream)), "moe_combine_rows_grad")
+    return tuple(out)
