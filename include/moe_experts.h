@@ -105,6 +105,44 @@ int moe_combine_rows_grad(const void* dout, const void* y, const int32_t* slot_r
                           int64_t rows, int32_t H, int32_t dout_type, int32_t y_type,
                           void* workspace, void* stream);
 
+/* ---- microscaled 4-bit floating point ----------------------------------------- */
+
+/* x [rows, K] of x_type (aligned to its elements) to codes and scales (format
+ * above), every byte of which is written.  rows >= 0, K >= 1. */
+int moe_mx4_quantize(const void* x, void* codes, void* scales, int64_t rows, int32_t K,
+                     int32_t x_type, void* stream);
+
+/* Weights as the rest of the library takes them, w [E, K, N] of w_type, to codes
+ * [E, N, 16 KB] and scales [E, N, KS] for moe_mx4_product: blocks along K, rows
+ * along N.  Done once, as the weights are loaded. */
+int moe_mx4_quantize_weights(const void* w, void* codes, void* scales, int32_t E, int32_t K,
+                             int32_t N, int32_t w_type, void* stream);
+
+/* The values that codes and scales stand for, to out [rows, K] of out_type
+ * (exact in both types). */
+int moe_mx4_dequantize(const void* codes, const void* scales, void* out, int64_t rows, int32_t K,
+                       int32_t out_type, void* stream);
+
+/* The experts' products.
+ *   a_codes, a_scales  device, a [a_rows, K] in mx4
+ *   w_codes, w_scales  device, w [E, N, K] in mx4
+ *   expert_offsets     device int32 [E + 1], as for moe_gemm2_combine
+ *   row_ids            device int32 [rows]: the row of a that each row takes (the
+ *                      dispatch gather: token_ids); NULL: row r takes a's row r.
+ *                      A row outside [0, a_rows) counts as zeros and is flagged as
+ *                      slot_rows entries are (with NULL: is zeros)
+ *   out                device bf16 [rows, N], or with swiglu != 0 (N even) [rows,
+ *                      N / 2]: silu(p[:, n]) * p[:, N / 2 + n] of the product p; rows
+ *                      from expert_offsets[E] on are not written
+ * Products are exact, sums are fp32, the activation is fp32, out is rounded
+ * once (to nearest even).  A NaN block makes the sums it enters NaN.  Pad
+ * bytes of scales are not used.  1 <= E <= 1024; the codes of a, and of one
+ * expert's weights, below 2 GiB each (else MOE_ERR_UNSUPPORTED). */
+int moe_mx4_product(const void* a_codes, const void* a_scales, const void* w_codes,
+                    const void* w_scales, const int32_t* expert_offsets, const int32_t* row_ids,
+                    void* out, int64_t a_rows, int64_t rows, int32_t K, int32_t N, int32_t E,
+                    int32_t swiglu, void* workspace, void* stream);
+
 /* ABI version of this header (major * 100 + minor): 100. */
 int moe_experts_abi_version(void);
 

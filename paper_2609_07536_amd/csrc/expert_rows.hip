@@ -5,6 +5,7 @@
 #include <cstddef>
 #include <cstdint>
 
+#include "expert_units.h"
 #include "moe_experts.h"
 #include "status_bits.h"
 
@@ -83,16 +84,6 @@ __device__ __forceinline__ void lds_put(uint32_t* p, uint32_t v) {
   __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
 }
 
-__device__ __forceinline__ uint32_t wave_prefix(uint32_t v) {   // inclusive, over the lanes
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t u = __shfl_up(v, d);
-    if (lane >= d) v += u;
-  }
-  return v;
-}
-
 // kParts: wave parts times experts that fit (a workgroup has as many waves as that allows)
 template <int kMaxThreads, int kParts, bool kOne>
 __global__ void __launch_bounds__(kMaxThreads) sort_place_kernel(SortArgs a) {
@@ -145,7 +136,7 @@ __global__ void __launch_bounds__(kMaxThreads) sort_place_kernel(SortArgs a) {
     const int e0 = min(lane * each, a.E), e1 = min(e0 + each, a.E);
     uint32_t n = 0;
     for (int e = e0; e < e1; ++e) n += first[e];
-    const uint32_t end = wave_prefix(n);
+    const uint32_t end = (uint32_t)wave_prefix((int)n);
     uint32_t at = end - n;
     for (int e = e0; e < e1; ++e) {
       const uint32_t c = first[e];

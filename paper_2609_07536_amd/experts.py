@@ -19,7 +19,8 @@ from .binding import lib as _base_lib
 
 EXPORTED = (
     "moe_sort_scratch_size", "moe_sort_by_expert", "moe_dispatch_rows", "moe_dispatch_rows_grad",
-    "moe_combine_rows", "moe_combine_rows_grad", "moe_experts_abi_version",
+    "moe_combine_rows", "moe_combine_rows_grad", "moe_mx4_quantize", "moe_mx4_quantize_weights",
+    "moe_mx4_dequantize", "moe_mx4_product", "moe_experts_abi_version",
 )
 
 _TYPES = {torch.bfloat16: 0, torch.float32: 1}   # moe_type_t
@@ -39,6 +40,10 @@ def lib() -> ctypes.CDLL:
         L.moe_dispatch_rows_grad.argtypes = [vp] * 3 + [i32, i32, i64, i32, i32, i32, vp, vp]
         L.moe_combine_rows.argtypes = [vp] * 4 + [i32, i32, i64, i32, i32, i32, vp, vp]
         L.moe_combine_rows_grad.argtypes = [vp] * 6 + [i32, i32, i64, i32, i32, i32, vp, vp]
+        L.moe_mx4_quantize.argtypes = [vp] * 3 + [i64, i32, i32, vp]
+        L.moe_mx4_quantize_weights.argtypes = [vp] * 3 + [i32, i32, i32, i32, vp]
+        L.moe_mx4_dequantize.argtypes = [vp] * 3 + [i64, i32, i32, vp]
+        L.moe_mx4_product.argtypes = [vp] * 7 + [i64, i64, i32, i32, i32, i32, vp, vp]
         for name in EXPORTED:
             if name != "moe_sort_scratch_size":
                 getattr(L, name).restype = ctypes.c_int
@@ -190,3 +195,96 @@ def combine_rows_grad(d_out, y, slot_rows, gates, out=None, workspace: Optional[
                                       _TYPES[d_out.dtype], _TYPES[y.dtype], _status_word(workspace),
                                       _stream(stream)), "moe_combine_rows_grad")
     return tuple(out)
+
+
+# ---- microscaled 4-bit floating point -----------------------------------------------
+
+class MX4(NamedTuple):
+    """A tensor [..., K] in microscaled 4-bit floating point: codes uint8
+    [..., 16 ceil(K / 32)], scales uint8 [..., 4 ceil(K / 128)], K elements a
+    row (the layout: include/moe_experts.h)."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    K: int
+
+
+def _mx4_shapes(lead, K):
+    blocks = -(-K // 32)
+    return (*lead, 16 * blocks), (*lead, (blocks + 3) // 4 * 4)
+
+
+def _mx4_out(out, lead, K, device, stream):
+    codes, scales = _mx4_shapes(lead, K)
+    if out is None:
+        return MX4(_empty(codes, torch.uint8, device, stream), _empty(scales, torch.uint8, device, stream), K)
+    _mx4_check(out, "out", lead)
+    if out.K != K:
+        raise TypeError(f"out: K is {out.K}, expected {K}")
+    return out
+
+
+def _mx4_check(m, what, lead):
+    codes, scales = _mx4_shapes(lead, m.K)
+    _check(m.codes, what + ".codes", codes, torch.uint8)
+    _check(m.scales, what + ".scales", scales, torch.uint8)
+
+
+def mx4_quantize(x, out: Optional[MX4] = None, stream=None) -> MX4:
+    """moe_mx4_quantize: x [..., K], bf16 or fp32."""
+    _check(x, "x", x.shape, torch.bfloat16, torch.float32)
+    if x.dim() < 1:
+        raise TypeError("x: expected at least one dimension")
+    K, lead = x.shape[-1], x.shape[:-1]
+    out = _mx4_out(out, lead, K, x.device, stream)
+    _done(lib().moe_mx4_quantize(x.data_ptr(), out.codes.data_ptr(), out.scales.data_ptr(), lead.numel(), K,
+                                 _TYPES[x.dtype], _stream(stream)), "moe_mx4_quantize")
+    return out
+
+
+def mx4_quantize_weights(w, out: Optional[MX4] = None, stream=None) -> MX4:
+    """moe_mx4_quantize_weights: w [E, K, N] (bf16 or fp32, the layout of w2 and of
+    w_gate_up) to the MX4 [E, N, K] that mx4_product reads."""
+    _check(w, "w", w.shape, torch.bfloat16, torch.float32)
+    if w.dim() != 3:
+        raise TypeError(f"w: expected [E, K, N], got {tuple(w.shape)}")
+    E, K, N = w.shape
+    out = _mx4_out(out, (E, N), K, w.device, stream)
+    _done(lib().moe_mx4_quantize_weights(w.data_ptr(), out.codes.data_ptr(), out.scales.data_ptr(), E, K, N,
+                                         _TYPES[w.dtype], _stream(stream)), "moe_mx4_quantize_weights")
+    return out
+
+
+def mx4_dequantize(m: MX4, out=None, dtype=torch.bfloat16, stream=None):
+    """moe_mx4_dequantize: the values of `m` [..., K] as bf16 or fp32 (exact in both)."""
+    lead = m.codes.shape[:-1]
+    _mx4_check(m, "m", lead)
+    if out is None:
+        out = _empty((*lead, m.K), dtype, m.codes.device, stream)
+    _check(out, "out", (*lead, m.K), torch.bfloat16, torch.float32)
+    _done(lib().moe_mx4_dequantize(m.codes.data_ptr(), m.scales.data_ptr(), out.data_ptr(), lead.numel(), m.K,
+                                   _TYPES[out.dtype], _stream(stream)), "moe_mx4_dequantize")
+    return out
+
+
+def mx4_product(a: MX4, w: MX4, expert_offsets, rows: int, row_ids=None, swiglu: bool = False, out=None,
+                workspace: Optional[Workspace] = None, stream=None):
+    """moe_mx4_product: a [a_rows, K] and w [E, N, K] to bf16 [rows, N], or with
+    swiglu [rows, N / 2]; row_ids int32 (at least `rows`): the row of `a` that
+    each row takes.  Rows from expert_offsets[E] on are not written."""
+    if a.codes.dim() != 2 or w.codes.dim() != 3 or a.K != w.K:
+        raise TypeError(f"expected a [rows, K] and w [E, N, K], got {tuple(a.codes.shape)}, K = {a.K}, and "
+                        f"{tuple(w.codes.shape)}, K = {w.K}")
+    a_rows, (E, N) = a.codes.shape[0], w.codes.shape[:2]
+    _mx4_check(a, "a", (a_rows,))
+    _mx4_check(w, "w", (E, N))
+    _check(expert_offsets, "expert_offsets", (E + 1,), torch.int32)
+    if row_ids is not None:
+        _check(row_ids, "row_ids", row_ids.shape, torch.int32)
+    if rows > (row_ids.numel() if row_ids is not None else a_rows):
+        raise TypeError(f"{rows} rows of {a_rows}" + (f", {row_ids.numel()} row_ids" if row_ids is not None else ""))
+    out = _output(out, "out", (rows, N // 2 if swiglu else N), a.codes.device, stream, torch.bfloat16)
+    _done(lib().moe_mx4_product(a.codes.data_ptr(), a.scales.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr(),
+                                expert_offsets.data_ptr(), row_ids.data_ptr() if row_ids is not None else None,
+                                out.data_ptr(), a_rows, rows, a.K, N, E, int(swiglu), _status_word(workspace),
+                                _stream(stream)), "moe_mx4_product")
+    return out
