@@ -62,14 +62,20 @@ __device__ __forceinline__ ExpertUnit find_expert(const ExpertRows<K>& r, int e0
           __builtin_amdgcn_readlane(n, l)};
 }
 
-__device__ __forceinline__ int wave_prefix(int v) {   // inclusive, over the lanes
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int u = __shfl_up(v, d);
-    if (lane >= d) v += u;
-  }
-  return v;
+// Inclusive, over the lanes: within rows of 16 by shifts, then each row's sum to the
+// next one's and the first half's to the second's (data-parallel primitives: each
+// step is one addition, where a shuffle through LDS takes 100 cycles).
+template <int kCtrl, int kRows>
+__device__ __forceinline__ int prefix_step(int v) {
+  return v + __builtin_amdgcn_update_dpp(0, v, kCtrl, kRows, 0xf, false);
+}
+__device__ __forceinline__ int wave_prefix(int v) {
+  v = prefix_step<0x111, 0xf>(v);   // row_shr 1, 2, 4, 8
+  v = prefix_step<0x112, 0xf>(v);
+  v = prefix_step<0x114, 0xf>(v);
+  v = prefix_step<0x118, 0xf>(v);
+  v = prefix_step<0x142, 0xa>(v);   // row_bcast 15 into rows 1 and 3
+  return prefix_step<0x143, 0xc>(v);   // row_bcast 31 into rows 2 and 3
 }
 
 struct SmallUnit {

@@ -5,6 +5,7 @@
 #include <cstddef>
 #include <cstdint>
 #include <type_traits>
+#include <utility>
 
 #include "expert_units.h"
 #include "lds_loads.h"
@@ -15,12 +16,14 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kBlock = 32;         // elements that share a scale
 constexpr int kBlockBytes = 16;    // their codes
+constexpr int kMaxExperts = 1024;
 
 __host__ __device__ inline int blocks_of(int K) { return (K + kBlock - 1) / kBlock; }
 __host__ __device__ inline int scale_pitch(int K) { return (blocks_of(K) + 3) / 4 * 4; }
@@ -70,16 +73,17 @@ __device__ __forceinline__ void load8(const T* p, int n, float (&v)[8]) {
     for (int i = 0; i < 8; ++i) v[i] = i < n ? (float)p[i] : 0.f;
   }
 }
-template <class T>
-__device__ __forceinline__ void store8(T* p, int n, const float (&v)[8]) {
-  if (n >= 8) {
-    T __attribute__((ext_vector_type(8))) x;
+// V values to p[0..min(n, V))
+template <int V, class T>
+__device__ __forceinline__ void store_few(T* p, int n, const float (&v)[8]) {
+  if (n >= V) {
+    T __attribute__((ext_vector_type(V))) x;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = (T)v[i];
-    *(typename Mem<T, 8>::type*)p = x;
+    for (int i = 0; i < V; ++i) x[i] = (T)v[i];
+    *(typename Mem<T, V>::type*)p = x;
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < V; ++i)
       if (i < n) p[i] = (T)v[i];
   }
 }
@@ -209,7 +213,7 @@ __global__ void __launch_bounds__(256) mx4_dequantize_kernel(const uint8_t* code
   float v[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) v[j] = byte == 255 ? __builtin_nanf("") : a[j >> 1][j & 1];
-  store8(out + row * K + 8 * c, K - 8 * c, v);
+  store_few<8>(out + row * K + 8 * c, K - 8 * c, v);
 }
 
 // ---- the experts' products -------------------------------------------------------
@@ -236,192 +240,523 @@ struct MxArgs {
   int NT;                    // tiles along them
 };
 
-// BM rows by BN weight rows, WM x WN waves, a ring of S stages
-template <int BM_, int BN_, int WM_, int WN_, int S_>
+// z / (1 + exp(-z)) by the reciprocal instruction (1 ulp): a full division is ten
+// instructions of each output.
+__device__ __forceinline__ float silu(float z) { return z * __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
+
+// BM rows by BN weight rows, WM x WN waves, a ring of four stages with D of them
+// ahead, R workgroups per CU.  Scales come 16 bytes of a row (four stages' worth, a
+// quad) at a time, with the first stage that they are for.
+template <int BM_, int BN_, int WM_, int WN_, int D_, int R_>
 struct MxTile {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, S = S_;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, D = D_, R = R_;
+  static constexpr int S = 4;
   static constexpr int NW = WM * WN, kThr = NW * 64;
-  static constexpr int MB = BM / WM / 32, NB = BN / WN / 32;   // a wave's 32 x 32 blocks
+  static constexpr int MB = BM / WM / 16, NB = BN / WN / 16;   // a wave's 16 x 16 blocks
+  static constexpr int LA = MB > 4 ? 3 : MB / 2;               // blocks of a that are read ahead
   static constexpr int kRows = BM + BN;
   static constexpr int kStage = kRows * 64;                    // bytes: 4 blocks of each row
   static constexpr int LPS = kStage / 1024 / NW;               // 1 KB loads per wave and stage
-  static constexpr int kSeg = 16;                              // stages whose scales are in LDS together
-  static constexpr int kScaleRow = kSeg * 4;                   // as many bytes as a stage's row
-  static constexpr int kScales = kRows * kScaleRow;
-  static_assert(kStage % (1024 * NW) == 0 && MB >= 1 && NB >= 1, "loads per wave");
-  static_assert((S - 2) * LPS <= 63 && S >= 2, "vmcnt range");
-  static_assert(S * kStage + kScales <= 160 * 1024, "LDS");
+  static constexpr int kQuad = kRows * 16;                     // bytes of scales of four stages
+  static constexpr int QL = kRows / 64;                        // 1 KB loads of a quad
+  static constexpr int SL = (QL + NW - 1) / NW;                // ... per wave (the last ones twice)
+  static constexpr int kScales = S * kStage;                   // two quads
+  static constexpr int kIds = kScales + 2 * kQuad;             // the next tile's rows of a
+  static constexpr int kLds = kIds + BM * 4;
+  // loads of a wave that stage j adds (j % 4 matters)
+  static constexpr int loads(int j) { return LPS + (j % 4 == 0 ? SL : 0); }
+  // loads after stage j + 1's while stage j is multiplied
+  static constexpr int newer(int j) { return (D > 2 ? loads(j + 2) : 0) + (D > 3 ? loads(j + 3) : 0); }
+  static_assert(D >= 2 && D <= S, "ring");
+  static_assert(BM % (16 * NW) == 0 && BN % (16 * NW) == 0 && BM % 64 == 0 && BN % 64 == 0, "loads per wave");
+  static_assert(BM <= 256, "one load of row ids");
+  static_assert(MB % 2 == 0 && NB % 2 == 0, "blocks");
+  static_assert(S * LPS + SL <= 63, "vmcnt range");
+  static_assert(R * (kLds + 4 * (kMaxExperts + 2)) <= 160 * 1024, "LDS");
 };
 
-// Position of 16-byte chunk c (0..3) of row r within the row's 64 bytes: the 16
-// rows that a read touches at once then fall on distinct banks.
-__device__ __forceinline__ int swz(int r, int c) { return c ^ ((r >> 2) & 3); }
+// Position of 16-byte chunk c (0..3) of a row within the row's 64 bytes, by two bits q
+// of the row.  A 16-byte read is served to 16 lanes at a time, lanes 0-3, 12-15, 20-23
+// and 24-27 first; with lane = i + 16 c and q = i / 4 these fall on distinct banks
+// (measured: 4.7 cycles an instruction, as for a linear read; 8.4 with c ^ q).
+__device__ __forceinline__ int swz(int q, int c) { return c ^ (((q ^ (q << 1)) & 2) | ((q >> 1) & 1)); }
 
 typedef const __attribute__((address_space(3))) uint8_t lds_u8;
 typedef const __attribute__((address_space(3))) u32x4 lds_u32x4;
 typedef const __attribute__((address_space(3))) uint32_t lds_u32;
 
+// f(0) .. f(N - 1), the index as a constant
+template <int N, class F, int... I>
+__device__ __forceinline__ void static_for_each(F& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>()), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void static_for(F f) {
+  static_for_each<N>(f, std::make_integer_sequence<int, N>());
+}
+
+// (Whole numbers only: copies of a bool and its padding end up in memory.)
+struct Tile {
+  int e, r0, rows_valid, n0, ok;
+};
+template <int BM>
+__device__ __forceinline__ int tiles_of(int r0, int r1) { return (max(r1 - r0, 0) + BM - 1) / BM; }
+// Tile `unit` (expert -> columns -> rows), by each wave for itself; row(i), i <= E:
+// expert i's first row (row(E): the end of the last one).
+template <int BM, int BNO, class Row>
+__device__ __forceinline__ Tile unit_at(const MxArgs& a, int unit, Row row) {
+  const int lane = threadIdx.x & 63;
+  int before = 0;   // tiles of the experts up to e0
+  for (int e0 = 0;; e0 += 64) {
+    const int r0 = row(min(e0 + lane, a.E)), r1 = row(min(e0 + lane + 1, a.E));
+    const int t = tiles_of<BM>(r0, r1), end = before + wave_prefix(t);
+    const uint64_t past = __ballot((long long)end * a.NT > unit);
+    if (past == 0) {
+      if (e0 + 64 >= a.E) return {0, 0, 0, 0, 0};
+      before = __builtin_amdgcn_readlane(end, 63);
+      continue;
+    }
+    const int i = (int)__builtin_ctzll(past);
+    const int n = __builtin_amdgcn_readlane(t, i), within = unit - (__builtin_amdgcn_readlane(end, i) - n) * a.NT;
+    const int nt = within / n, mi = within - nt * n;
+    const int start = __builtin_amdgcn_readlane(r0, i) + mi * BM;
+    return {e0 + i, start, min(BM, __builtin_amdgcn_readlane(r1, i) - start), nt * BNO, 1};
+  }
+}
+// All tiles of rows.  Offsets are clamped as in ExpertRows; bad ones are flagged.
+template <int BM>
+__device__ __forceinline__ int all_tiles(const MxArgs& a) {
+  const int lane = threadIdx.x & 63, cap = (int)a.rows;
+  int tiles = 0;
+  bool bad = false;
+  for (int e0 = 0; e0 < a.E; e0 += 64) {
+    const int e = e0 + lane, o0 = a.offsets[min(e, a.E)], o1 = a.offsets[min(e + 1, a.E)];
+    bad |= (e == 0 && o0 != 0) || o1 < o0 || o1 > cap;
+    tiles += __builtin_amdgcn_readlane(wave_prefix(tiles_of<BM>(min(max(o0, 0), cap), min(max(o1, 0), cap))), 63);
+  }
+  if (bad && a.status && blockIdx.x == 0)
+    __hip_atomic_fetch_or(a.status, kStBadRouting, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return tiles;
+}
+
 template <class C, bool kSwiglu>
-__global__ void __launch_bounds__(C::kThr) mx4_product_kernel(MxArgs a) {
-  __shared__ __align__(1024) uint8_t smem[C::S * C::kStage + C::kScales];
+__global__ void __launch_bounds__(C::kThr, C::R * C::NW / 4) mx4_product_kernel(MxArgs a) {
+#define MX_INLINE __attribute__((always_inline))
+  __shared__ __align__(1024) uint8_t smem[C::kLds];
+  __shared__ int expert_row[kMaxExperts + 1];   // each expert's first row, for the tiles after the first
   constexpr int BNO = kSwiglu ? C::BN / 2 : C::BN;   // output columns of a tile
+  static_assert(!kSwiglu || C::NB % 4 == 0, "a wave has pairs of gate and of up blocks");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+  // this workgroup's tiles: every step-th of an XCD's contiguous share
+  const int units = all_tiles<C::BM>(a) * a.NT, share = (units + 7) >> 3;
+  const int step = gridDim.x >> 3;
+  int unit = (blockIdx.x & 7) * share + (blockIdx.x >> 3);
+  const int last = min(((int)(blockIdx.x & 7) + 1) * share, units);
+  if (unit >= last) return;
+  auto row_at = [&](int e) MX_INLINE { return min(max(a.offsets[e], 0), (int)a.rows); };
+  Tile u = unit_at<C::BM, BNO>(a, unit, row_at);
+  for (int e = threadIdx.x; e <= a.E; e += C::kThr) expert_row[e] = row_at(e);
+
+  const uint32_t lds = lds_addr(smem);
+  lds_u8* base = (lds_u8*)(uintptr_t)lds;
+  const uint32_t pitch = (uint32_t)a.KB * kBlockBytes;
+  const int KT = (a.KB + 3) / 4;
+  const i32x4 ra = buffer_rsrc(a.a, (long long)a.a_rows * pitch), ras = buffer_rsrc(a.as, (long long)a.a_rows * a.KS);
+  const i32x4 rids = buffer_rsrc(a.row_ids, a.row_ids ? a.rows * 4 : 0);
+  i32x4 rw, rws;
+
+  auto issue_ids = [&](const Tile& t) MX_INLINE {   // a tile's row ids, four a lane
+    if (a.row_ids && wave == 0 && 4 * lane < C::BM)
+      dma16(rids, 4 * lane < t.rows_valid ? 4u * (uint32_t)(t.r0 + 4 * lane) : kOutOfRange, lds + C::kIds);
+  };
+  // tile row i (BM rows of a, then BN of w) to its row in memory, or -1
+  auto row_of = [&](const Tile& t, int i) MX_INLINE -> int {
+    if (i < C::BM) {
+      if (i >= t.rows_valid) return -1;
+      const int id = a.row_ids ? *(const __attribute__((address_space(3))) int*)(base + C::kIds + 4 * i) : t.r0 + i;
+      if (id >= 0 && id < a.a_rows) return id;
+      if (a.status) __hip_atomic_fetch_or(a.status, kStBadRouting, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      return -1;
+    }
+    const int j = i - C::BM;
+    if (!kSwiglu) return t.n0 + j < a.N ? t.n0 + j : -1;
+    const int n = t.n0 + (j < BNO ? j : j - BNO);
+    return n < a.NO ? (j < BNO ? n : a.NO + n) : -1;
+  };
+  // This lane's part of its wave's loads: load q is 16 rows of a stage, a's for the
+  // first ones; a load of scales is 64 rows of a quad.  Rows of a are swizzled by bits
+  // 2 and 3, rows of w by bits 3 and 4 (lw below).
+  constexpr int kLoadsA = C::BM / 16 / C::NW;
+  auto load_row = [&](int q, int ln) MX_INLINE { return (q * C::NW + wave) * 16 + (ln >> 2); };
+  auto load_chunk = [&](int q, int ln) MX_INLINE {
+    const int i = load_row(q, ln);
+    return swz((q < kLoadsA ? i >> 2 : i >> 3) & 3, ln & 3);
+  };
+  // (what is computed from this copy stays where it is used: hoisted out of the
+  // loops it would take the registers that the loop over K needs)
+  auto lane_here = [&]() MX_INLINE {
+    int v = lane;
+    asm volatile("" : "+v"(v));
+    return v;
+  };
+  auto scale_load = [&](int q) MX_INLINE { return (q * C::NW + wave) % C::QL; };
+  uint32_t off[C::LPS], soff[C::SL];
+  auto set_tile = [&](const Tile& t) MX_INLINE {
+    rw = buffer_rsrc(a.w + t.e * ((long long)a.N * pitch), (long long)a.N * pitch);
+    rws = buffer_rsrc(a.ws + (long long)t.e * a.N * a.KS, (long long)a.N * a.KS);
+    const int ln = lane_here();
+#pragma unroll
+    for (int q = 0; q < C::LPS; ++q) {
+      const int r = row_of(t, load_row(q, ln));
+      off[q] = r < 0 ? kOutOfRange : (uint32_t)r * pitch + load_chunk(q, ln) * kBlockBytes;
+    }
+#pragma unroll
+    for (int q = 0; q < C::SL; ++q) {
+      const int r = row_of(t, scale_load(q) * 64 + ln);
+      soff[q] = r < 0 ? kOutOfRange : (uint32_t)r * (uint32_t)a.KS;
+    }
+  };
+  // load q of stage kt, to its slot of the ring; what lies past the end is set out
+  // of range beforehand (cut_k) and loads zeros
+  const uint32_t ldsw = lds + (uint32_t)wave * 1024;
+  auto issue = [&](auto q, auto slot, uint32_t k) MX_INLINE {   // k: 64 bytes a stage, 0 past the end
+    constexpr int Q = decltype(q)::value;
+    dma16_at<decltype(slot)::value * C::kStage + Q * C::NW * 1024>(Q < kLoadsA ? ra : rw, off[Q], ldsw, k);
+  };
+  auto cut_k = [&](int kt) MX_INLINE {
+    const int ln = lane_here();
+#pragma unroll
+    for (int q = 0; q < C::LPS; ++q)
+      if (4 * kt + load_chunk(q, ln) >= a.KB) off[q] = kOutOfRange;
+  };
+  auto issue_scales = [&](int q, int kt) MX_INLINE {   // of the quad from stage kt on
+    const int i = scale_load(q);
+    const bool in = kt < KT;
+    dma16(64 * i < C::BM ? ras : rws, in ? soff[q] : kOutOfRange,
+          lds + (uint32_t)(C::kScales + ((kt >> 2) & 1) * C::kQuad + i * 1024), in ? 4u * (uint32_t)kt : 0);
+  };
+
+  const int wm0 = (wave / C::WN) * C::MB * 16, wn = wave % C::WN;
+  // first tile row of pair p of this wave's blocks of w: with SwiGLU half are gate, half up
+  auto w_row = [&](int p) MX_INLINE {
+    return C::BM + (kSwiglu ? (p < C::NB / 4 ? (wn * (C::NB / 4) + p) * 32 : BNO + (wn * (C::NB / 4) + p - C::NB / 4) * 32)
+                            : (wn * (C::NB / 2) + p) * 32);
+  };
+  const int l = lane & 15, g = lane >> 4;   // the instruction's row, and block of its 128 of K
+  // the row of its pair that a lane brings for block f of the two, so that its
+  // accumulators of both are columns 8 g .. 8 g + 7 of one output row
+  const int lw = 8 * (l >> 2) + (l & 3);
+  // where a lane's codes and scales are: a's and w's, plus constants (two bases for
+  // codes, an offset in an instruction ends at 64 KB)
+  const int wave_w = wn * (kSwiglu ? C::NB / 4 : C::NB / 2) * 32 + lw;   // (4 f rows leave bits 3, 4 alone)
+  lds_u8* const pa = base + (wm0 + l) * 64 + swz(l >> 2, g) * 16;
+  lds_u8* const pw = base + wave_w * 64 + swz(l >> 2, g) * 16;
+  // a lane without a block in the last stage has codes of zeros and takes the scale
+  // of the stage's first block, whatever pad bytes hold
+  const int back = 4 * (KT - 1) + g < a.KB ? 0 : g;
+  lds_u8 *qa, *qw;
+
+  // 16 bytes of codes and a scale: a lane's block of a 16-row operand
+  struct Frag {
+    u32x4 v;
+    int s;
+  };
+  // tile row of block nb of w, less what differs between waves and lanes
+  auto w_const = [](int nb) MX_INLINE {
+    const int p = nb >> 1;
+    return C::BM + (kSwiglu && p >= C::NB / 4 ? BNO + (p - C::NB / 4) * 32 : p * 32) + 4 * (nb & 1);
+  };
+  auto read_a = [&](int mb, int slot, int stage4) MX_INLINE -> Frag {   // stage4: of its quad
+    const int at = slot * C::kStage + mb * 1024;
+    return {*(lds_u32x4*)((at < 65536 ? pa : pa + 65536) + (at < 65536 ? at : at - 65536)), qa[stage4 * 4 + mb * 256]};
+  };
+  auto read_w = [&](int nb, int slot, int stage4) MX_INLINE -> Frag {
+    const int r = w_const(nb), at = slot * C::kStage + r * 64;
+    return {*(lds_u32x4*)((at < 65536 ? pw : pw + 65536) + (at < 65536 ? at : at - 65536)), qw[stage4 * 4 + r * 16]};
+  };
+
+  f32x4 acc[C::NB][C::MB];
+  Tile done = u;   // the tile in acc
+  done.ok = 0;
+  issue_ids(u);
+  for (;;) {
+    waitcnt_vm<0>();   // u's row ids (and loads past the end of the last tile, which write to LDS as well)
+    block_barrier();
+    if (u.ok) set_tile(u);
+    // The ring is free: u's first stages land while the last tile is stored, a load
+    // or two and then the stores of 16 of its rows (each lane's: eight neighbouring
+    // columns, 16 bytes, at a time).
+    constexpr int kFirst = C::D * C::LPS;
+    const int ln = lane_here();
+    static_for<C::MB>([&](auto m) MX_INLINE {
+      constexpr int mb = decltype(m)::value;
+      if (u.ok) {
+        if constexpr (mb == 0)
+#pragma unroll
+          for (int q = 0; q < C::SL; ++q) issue_scales(q, 0);
+        constexpr int i0 = mb * kFirst / C::MB, i1 = (mb + 1) * kFirst / C::MB;
+        static_for<i1 - i0>([&](auto i) MX_INLINE {
+          constexpr int at = i0 + decltype(i)::value, kt = at / C::LPS, q = at % C::LPS;
+          if (q == 0 && kt >= KT - 1) cut_k(kt);
+          issue(std::integral_constant<int, q>(), std::integral_constant<int, kt>(), kt < KT ? 64u * kt : 0);
+        });
+      }
+      const int row = wm0 + mb * 16 + (ln & 15);
+      if (done.ok && row < done.rows_valid) {
+        __bf16* o = a.out + (long long)(done.r0 + row) * a.NO;
+#pragma unroll
+        for (int p = 0; p < (kSwiglu ? C::NB / 4 : C::NB / 2); ++p) {
+          float v[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            v[i] = acc[2 * p + i / 4][mb][i % 4];
+            if (kSwiglu) v[i] = silu(v[i]) * acc[C::NB / 2 + 2 * p + i / 4][mb][i % 4];
+          }
+          const int n = done.n0 + w_row(p) - C::BM + 8 * (ln >> 4);
+          if (n < a.NO) store_few<8>(o + n, a.NO - n, v);
+        }
+      }
+    });
+    if (!u.ok) break;
+    Tile next = u;
+    unit += step;
+    next.ok = unit < last;
+    if (next.ok) next = unit_at<C::BM, BNO>(a, unit, [&](int e) MX_INLINE { return expert_row[e]; });
+#pragma unroll
+    for (int nb = 0; nb < C::NB; ++nb)
+#pragma unroll
+      for (int mb = 0; mb < C::MB; ++mb) acc[nb][mb] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    waitcnt_vm<(C::D - 1) * C::LPS>();   // stage 0 and its scales
+    block_barrier();
+    if (next.ok) issue_ids(next);   // (this tile's have been read)
+    // w's blocks of a stage stay in registers for it, a's come by one after the
+    // other, read LA ahead.  Once the last is on its way the stage's slot is free:
+    // the next stage goes out, and the first operands of stage kt + 1 are read, so that
+    // products are left to issue after the barrier, with the reads and loads spread
+    // between them.  Four stages at a time: slots, parities and places are
+    // constants, so that hardly a vector instruction is left beside the products
+    // (two waves share a SIMD's issue: 100 such instructions a stage cost a
+    // quarter of its time).
+    qa = base + C::kScales + (wm0 + l) * 16 + g - (KT == 1 ? back : 0);
+    qw = base + C::kScales + wave_w * 16 + g - (KT == 1 ? back : 0);
+    int other = C::kQuad;   // from this quad of scales to the next
+    Frag w[2][C::NB], x[C::MB];
+#pragma unroll
+    for (int nb = 0; nb < C::NB; ++nb) w[0][nb] = read_w(nb, 0, 0);
+#pragma unroll
+    for (int mb = 0; mb < C::LA; ++mb) x[mb] = read_a(mb, 0, 0);
+    auto stage = [&](auto pos, int kt) MX_INLINE {
+      constexpr int J = decltype(pos)::value, kNext = (J + 1) % 4, kLate = C::MB - C::LA;
+      if (kt + C::D >= KT - 1) cut_k(kt + C::D);
+      const uint32_t k = kt + C::D < KT ? 64u * (uint32_t)(kt + C::D) : 0;
+      static_for<C::MB>([&](auto m) MX_INLINE {
+        constexpr int mb = decltype(m)::value;
+        if constexpr (mb < kLate) {
+          x[mb + C::LA] = read_a(mb + C::LA, J % C::S, J);
+        } else {
+          if constexpr (mb == kLate) {   // the blocks from here on are multiplied after the barrier
+            // stage kt + 1 has landed, and this one's last reads
+            waitcnt_vm<C::newer(J)>();
+            block_barrier();
+            if ((J + C::D) % 4 == 0)
+#pragma unroll
+              for (int q = 0; q < C::SL; ++q) issue_scales(q, kt + C::D);
+            if (J == 3) qa += other, qw += other, other = -other;
+            if (kt + 1 == KT - 1) qa -= back, qw -= back;
+          }
+          x[mb - kLate] = read_a(mb - kLate, kNext % C::S, kNext);
+        }
+        static_for<C::NB>([&](auto n) MX_INLINE {
+          constexpr int nb = decltype(n)::value;
+          const Frag &p = w[J & 1][nb], &q = x[mb];
+          acc[nb][mb] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+              i32x8{(int)p.v[0], (int)p.v[1], (int)p.v[2], (int)p.v[3], 0, 0, 0, 0},
+              i32x8{(int)q.v[0], (int)q.v[1], (int)q.v[2], (int)q.v[3], 0, 0, 0, 0}, acc[nb][mb], 4, 4, 0, p.s, 0, q.s);
+          if constexpr (mb >= kLate) {   // (kSteps products: the next w, and the loads, spread over them)
+            constexpr int kSteps = C::LA * C::NB, i = (mb - kLate) * C::NB + nb;
+            constexpr int o0 = i * C::NB / kSteps, o1 = (i + 1) * C::NB / kSteps;
+            static_for<o1 - o0>([&](auto o) MX_INLINE { w[kNext & 1][o0 + o] = read_w(o0 + o, kNext % C::S, kNext); });
+            constexpr int q0 = i * C::LPS / kSteps, q1 = (i + 1) * C::LPS / kSteps;
+            static_for<q1 - q0>([&](auto o) MX_INLINE {
+              issue(std::integral_constant<int, q0 + decltype(o)::value>(), std::integral_constant<int, (J + C::D) % C::S>(), k);
+            });
+          }
+        });
+        __builtin_amdgcn_sched_barrier(0);   // (else the products all move behind the barrier)
+      });
+    };
+    for (int kt = 0;;) {
+      stage(std::integral_constant<int, 0>(), kt);
+      if (++kt >= KT) break;
+      stage(std::integral_constant<int, 1>(), kt);
+      if (++kt >= KT) break;
+      stage(std::integral_constant<int, 2>(), kt);
+      if (++kt >= KT) break;
+      stage(std::integral_constant<int, 3>(), kt);
+      if (++kt >= KT) break;
+    }
+    done = u;
+    u = next;
+  }
+#undef MX_INLINE
+}
+
+// ---- few rows per expert ------------------------------------------------------------
+//
+// Such a call reads each weight for a handful of rows: it is bound by the stream
+// of the weights, and at the smallest by how soon that stream starts.  So a
+// wave loads its weights straight into registers, all of 128 KC of K at once (16
+// weight rows, 64 bytes of each, an instruction), while the rows of a, shared
+// by the workgroup's waves, go to LDS; no ring, one barrier per segment.
+// The 16x16x128 instruction then takes 16 weight rows and 16 rows of a.
+
+__device__ __forceinline__ u32x4 buffer_load16(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, 0));
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t load_rsrc(const void* base, long long bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)(bytes > 0x7fffffffLL ? 0x7fffffffLL : bytes), 0x00020000);
+}
+
+// 16 MB rows of a; a wave's 32 weight rows (with SwiGLU 16 gate and 16 up ones);
+// NW waves; KC stages of 128 of K in registers at a time
+template <int MB_, int KC_, int NW_>
+struct MxThin {
+  static constexpr int MB = MB_, KC = KC_, NW = NW_, kThr = 64 * NW;
+  static constexpr int BM = 16 * MB, BN = 32 * NW;
+  static constexpr int kCodes = BM * 64 * KC;                       // LDS bytes
+  static constexpr int kSegs = (KC + 15) / 16, kScales = BM * 64 * kSegs;   // (64 bytes a row and 16 stages)
+  static_assert(KC * MB % NW == 0, "loads per wave");
+  static_assert(KC % 4 == 0, "scales are loaded 16 bytes at a time");
+};
+
+template <class C, bool kSwiglu>
+__global__ void __launch_bounds__(C::kThr) mx4_thin_kernel(MxArgs a) {
+  __shared__ __align__(1024) uint8_t smem[C::kCodes + C::kScales];
+  constexpr int BNO = kSwiglu ? C::BN / 2 : C::BN;
   int rows_dev;
   const SmallUnit u = small_unit<C::BM, BNO>(a.offsets, a.rows, a.E, a.NT, a.status, &rows_dev);
   if (!u.ok) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint32_t lds = lds_addr(smem), lds_s = lds + C::S * C::kStage;
+  const int l = lane & 15, g = lane >> 4;   // the instruction's row, and block of its 128 of K
+  const uint32_t lds = lds_addr(smem), lds_s = lds + C::kCodes;
   const long long pitch = (long long)a.KB * kBlockBytes;
   const i32x4 ra = buffer_rsrc(a.a, a.a_rows * pitch), ras = buffer_rsrc(a.as, (long long)a.a_rows * a.KS);
-  const i32x4 rw = buffer_rsrc(a.w + u.e * (a.N * pitch), a.N * pitch);
-  const i32x4 rws = buffer_rsrc(a.ws + (long long)u.e * a.N * a.KS, (long long)a.N * a.KS);
-
-  // tile row i (BM rows of a, then BN of w) to its row in memory, or -1
-  auto row_of = [&](int i) -> int {
-    if (i < C::BM) {
-      if (i >= u.rows_valid) return -1;
-      const int r = u.r0 + i;
-      if (!a.row_ids) return r < a.a_rows ? r : -1;
-      const int id = a.row_ids[r];
-      if (id < 0 || id >= a.a_rows) {
-        if (a.status) __hip_atomic_fetch_or(a.status, kStBadRouting, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        return -1;
-      }
-      return id;
-    }
-    const int j = i - C::BM;
-    if (!kSwiglu) return u.n0 + j < a.N ? u.n0 + j : -1;
-    const int n = u.n0 + (j < BNO ? j : j - BNO);
-    return n < a.NO ? (j < BNO ? n : a.NO + n) : -1;
-  };
-  // this lane's part of its wave's loads: a load is 16 rows of a stage
-  uint32_t off[C::LPS], soff[C::LPS];
-  int chunk[C::LPS];
-#pragma unroll
-  for (int q = 0; q < C::LPS; ++q) {
-    const int i = (C::LPS * wave + q) * 16 + (lane >> 2), r = row_of(i);
-    chunk[q] = swz(i, lane & 3);
-    off[q] = r < 0 ? kOutOfRange : (uint32_t)(r * pitch) + chunk[q] * kBlockBytes;
-    // (scales: the same rows in the same order, 16 bytes of a row's 64 a lane)
-    soff[q] = r < 0 ? kOutOfRange : (uint32_t)((long long)r * a.KS) + chunk[q] * 16;
-  }
+  const auto rw = load_rsrc(a.w + u.e * (a.N * pitch), a.N * pitch);
+  const auto rws = load_rsrc(a.ws + (long long)u.e * a.N * a.KS, (long long)a.N * a.KS);
   const int KT = (a.KB + 3) / 4;
-  auto issue = [&](int kt, int slot) {
-#pragma unroll
-    for (int q = 0; q < C::LPS; ++q) {
-      const bool in = off[q] != kOutOfRange && 4 * kt + chunk[q] < a.KB;
-      const int i = (C::LPS * wave + q) * 16;   // uniform: a's rows or w's
-      dma16(i < C::BM ? ra : rw, in ? off[q] + 64u * (uint32_t)kt : kOutOfRange,
-            lds + (uint32_t)(slot * C::kStage + i * 64));
-    }
-  };
-  auto issue_scales = [&](int seg) {
-#pragma unroll
-    for (int q = 0; q < C::LPS; ++q) {
-      const uint32_t k = (uint32_t)(seg * C::kScaleRow);
-      const bool in = soff[q] != kOutOfRange && (int)k + chunk[q] * 16 < a.KS;
-      const int i = (C::LPS * wave + q) * 16;
-      dma16(i < C::BM ? ras : rws, in ? soff[q] + k : kOutOfRange, lds_s + (uint32_t)(i * 64));
-    }
-  };
 
-  const int wm0 = (wave / C::WN) * C::MB * 32, wn = wave % C::WN;
-  // tile rows of this wave's block of w: with SwiGLU its first half gate, the other up
-  auto w_row = [&](int nb) {
-    return kSwiglu ? (nb < C::NB / 2 ? (wn * (C::NB / 2) + nb) * 32 : BNO + (wn * (C::NB / 2) + nb - C::NB / 2) * 32)
-                   : (wn * C::NB + nb) * 32;
-  };
-  const int h = lane >> 5, l = lane & 31;
-  // the row of w that a lane brings as row l of the instruction, so that its
-  // accumulators 8c .. 8c + 7 are columns 16c + 8h .. of one output row
-  const int lw = 16 * (l >> 4) + 8 * ((l >> 2) & 1) + 4 * ((l >> 3) & 1) + (l & 3);
-  const uint32_t tail = (a.KB & 3) ? (1u << (8 * (a.KB & 3))) - 1 : ~0u;   // scales of the last stage
-
-  f32x16 acc[C::NB][C::MB];
-#pragma unroll
-  for (int nb = 0; nb < C::NB; ++nb)
-#pragma unroll
-    for (int mb = 0; mb < C::MB; ++mb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[nb][mb][i] = 0.f;
-
-  issue_scales(0);
-#pragma unroll
-  for (int s = 0; s < C::S - 1; ++s) issue(s, s);
-  int slot = 0;
-  for (int kt = 0; kt < KT; ++kt) {
-    waitcnt_vm<(C::S - 2) * C::LPS>();
-    block_barrier();
-    if (kt > 0 && kt % C::kSeg == 0) {   // the next segment's scales (a reduction over 2048)
-      issue_scales(kt / C::kSeg);
-      waitcnt_vm<0>();
-      block_barrier();
-    }
-    issue(kt + C::S - 1, (slot + C::S - 1) % C::S);   // (past the end: nothing is read)
-    lds_u8* base = (lds_u8*)(uintptr_t)(lds + (uint32_t)(slot * C::kStage));
-    lds_u8* sbase = (lds_u8*)(uintptr_t)lds_s;
-    const uint32_t mask = kt == KT - 1 ? tail : ~0u;
-    const int sc = (kt % C::kSeg) >> 2, sb = (kt & 3) * 4;   // the stage's dword of a scale row
-    uint32_t sa[C::MB], sw[C::NB];
-#pragma unroll
-    for (int mb = 0; mb < C::MB; ++mb) {
-      const int r = wm0 + mb * 32 + l;
-      sa[mb] = (*(lds_u32*)(sbase + r * 64 + swz(r, sc) * 16 + sb) & mask) >> (8 * h);
-    }
-#pragma unroll
-    for (int nb = 0; nb < C::NB; ++nb) {
-      const int r = C::BM + w_row(nb) + lw;
-      sw[nb] = (*(lds_u32*)(sbase + r * 64 + swz(r, sc) * 16 + sb) & mask) >> (8 * h);
-    }
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      i32x8 fa[C::MB], fw[C::NB];
-#pragma unroll
-      for (int mb = 0; mb < C::MB; ++mb) {
-        const int r = wm0 + mb * 32 + l;
-        const u32x4 v = *(lds_u32x4*)(base + r * 64 + swz(r, 2 * ks + h) * 16);
-        fa[mb] = i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0};
-      }
-#pragma unroll
-      for (int nb = 0; nb < C::NB; ++nb) {
-        const int r = C::BM + w_row(nb) + lw;
-        const u32x4 v = *(lds_u32x4*)(base + r * 64 + swz(r, 2 * ks + h) * 16);
-        fw[nb] = i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0};
-      }
-#pragma unroll
-      for (int nb = 0; nb < C::NB; ++nb)
-#pragma unroll
-        for (int mb = 0; mb < C::MB; ++mb)
-          acc[nb][mb] = ks == 0 ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fw[nb], fa[mb], acc[nb][mb], 4, 4, 0,
-                                                                                   (int)sw[nb], 0, (int)sa[mb])
-                                : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fw[nb], fa[mb], acc[nb][mb], 4, 4, 2,
-                                                                                   (int)sw[nb], 2, (int)sa[mb]);
-    }
-    slot = slot + 1 == C::S ? 0 : slot + 1;
-  }
-  waitcnt_vm<0>();   // (the loads past the end write to LDS as well)
-
-  // each lane's rows: eight columns, one 16-byte store, at a time
+  // a's rows for this lane's LDS loads (16 rows, 64 bytes of each, a load)
+  uint32_t off[C::MB], soff[C::MB];
+  const int ca = swz(lane >> 4, lane & 3);
 #pragma unroll
   for (int mb = 0; mb < C::MB; ++mb) {
-    const int row = wm0 + mb * 32 + l;
-    if (row >= u.rows_valid) continue;
-    __bf16* o = a.out + (long long)(u.r0 + row) * a.NO;
-#pragma unroll
-    for (int nb = 0; nb < (kSwiglu ? C::NB / 2 : C::NB); ++nb)
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        float v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          v[i] = acc[nb][mb][8 * c + i];
-          if (kSwiglu) {
-            const float up = acc[nb + C::NB / 2][mb][8 * c + i];
-            v[i] = v[i] / (1.f + __expf(-v[i])) * up;
-          }
-        }
-        const int n = u.n0 + (kSwiglu ? (wn * (C::NB / 2) + nb) * 32 : w_row(nb)) + 16 * c + 8 * h;
-        if (n < a.NO) store8(o + n, a.NO - n, v);
+    const int i = 16 * mb + (lane >> 2);
+    int r = -1;
+    if (i < u.rows_valid) {
+      r = u.r0 + i;
+      if (a.row_ids) {
+        r = a.row_ids[r];
+        if ((r < 0 || r >= a.a_rows) && a.status)
+          __hip_atomic_fetch_or(a.status, kStBadRouting, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
+      if (r >= a.a_rows) r = -1;
+    }
+    off[mb] = r < 0 ? kOutOfRange : (uint32_t)(r * pitch) + ca * kBlockBytes;
+    soff[mb] = r < 0 ? kOutOfRange : (uint32_t)((long long)r * a.KS) + ca * 16;
+  }
+  // this lane's weight rows: block f's instruction row l.  Plain: columns 8 (l / 4) +
+  // 4 f + l % 4 of the wave's 32, so that a lane ends up with 8 neighbouring ones
+  const int n0 = u.n0 + wave * (BNO / C::NW);
+  uint32_t woff[2], wsoff[2];
+#pragma unroll
+  for (int f = 0; f < 2; ++f) {
+    const int n = n0 + (kSwiglu ? l : 8 * (l >> 2) + 4 * f + (l & 3));
+    const int r = kSwiglu && f ? a.NO + n : n;
+    woff[f] = n < a.NO ? (uint32_t)(r * pitch) + g * kBlockBytes : kOutOfRange;
+    wsoff[f] = n < a.NO ? (uint32_t)((long long)r * a.KS) : kOutOfRange;
+  }
+  const uint32_t tail = (a.KB & 3) ? (1u << (8 * (a.KB & 3))) - 1 : ~0u;   // scales of the last stage
+
+  f32x4 acc[2][C::MB];
+#pragma unroll
+  for (int f = 0; f < 2; ++f)
+#pragma unroll
+    for (int mb = 0; mb < C::MB; ++mb) acc[f][mb] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  lds_u8* base = (lds_u8*)(uintptr_t)lds;
+  lds_u8* sbase = (lds_u8*)(uintptr_t)lds_s;
+  for (int kt0 = 0; kt0 < KT; kt0 += C::KC) {
+    if (kt0) block_barrier();   // the segment before has been read
+#pragma unroll
+    for (int j = 0; j < C::KC * C::MB / C::NW; ++j) {
+      const int q = wave + C::NW * j;
+      const int mb = q % C::MB, kt = kt0 + q / C::MB;   // (uniform)
+      uint32_t o = off[0];
+#pragma unroll
+      for (int i = 1; i < C::MB; ++i) o = mb == i ? off[i] : o;
+      dma16(ra, o != kOutOfRange && 4 * kt + ca < a.KB ? o + 64u * (uint32_t)kt : kOutOfRange,
+            lds + (uint32_t)((q / C::MB * C::MB + mb) * 1024));
+    }
+    for (int q = wave; q < C::kSegs * C::MB; q += C::NW) {
+      const int mb = q % C::MB, seg = q / C::MB;   // 64 bytes of scales a row: 16 stages
+      uint32_t o = soff[0];
+#pragma unroll
+      for (int i = 1; i < C::MB; ++i) o = mb == i ? soff[i] : o;
+      const int k = 4 * kt0 + 64 * seg;
+      if (C::KC >= 16 || 4 * ca < C::KC)   // (lanes past a shorter segment: not in LDS)
+        dma16(ras, o != kOutOfRange && k + 16 * ca < a.KS ? o + (uint32_t)k : kOutOfRange, lds_s + (uint32_t)(q * 1024));
+    }
+    u32x4 w[2][C::KC], ws[2][C::KC / 4];
+#pragma unroll
+    for (int f = 0; f < 2; ++f) {
+#pragma unroll
+      for (int k = 0; k < C::KC / 4; ++k)
+        ws[f][k] = buffer_load16(rws, wsoff[f] != kOutOfRange && 4 * (kt0 + 4 * k) < a.KS ? wsoff[f] + 4u * (uint32_t)(kt0 + 4 * k) : kOutOfRange);
+    }
+#pragma unroll
+    for (int k = 0; k < C::KC; ++k)
+#pragma unroll
+      for (int f = 0; f < 2; ++f)
+        w[f][k] = buffer_load16(rw, woff[f] != kOutOfRange && 4 * (kt0 + k) + g < a.KB ? woff[f] + 64u * (uint32_t)(kt0 + k) : kOutOfRange);
+    waitcnt_vm<2 * C::KC + 2 * (C::KC / 4)>();   // a's loads, which were issued first
+    block_barrier();
+#pragma unroll
+    for (int k = 0; k < C::KC; ++k) {
+      if (kt0 + k >= KT) break;
+      const uint32_t mask = kt0 + k == KT - 1 ? tail : ~0u;
+      int sw[2];
+#pragma unroll
+      for (int f = 0; f < 2; ++f) sw[f] = (int)((ws[f][k / 4][k % 4] & mask) >> (8 * g));
+#pragma unroll
+      for (int mb = 0; mb < C::MB; ++mb) {
+        const u32x4 v = *(lds_u32x4*)(base + (k * C::MB + mb) * 1024 + l * 64 + swz(l >> 2, g) * 16);
+        const uint32_t s = *(lds_u32*)(sbase + (k / 16 * C::MB + mb) * 1024 + l * 64 + swz(l >> 2, (k % 16) / 4) * 16 + 4 * (k % 4));
+        const i32x8 fa = {(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0};
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+          const i32x8 fw = {(int)w[f][k][0], (int)w[f][k][1], (int)w[f][k][2], (int)w[f][k][3], 0, 0, 0, 0};
+          acc[f][mb] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw, fa, acc[f][mb], 4, 4, 0, sw[f], 0,
+                                                                        (int)((s & mask) >> (8 * g)));
+        }
+      }
+    }
+  }
+
+#pragma unroll
+  for (int mb = 0; mb < C::MB; ++mb) {
+    const int row = 16 * mb + l;
+    if (row >= u.rows_valid) continue;
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float x = acc[0][mb][i], y = acc[1][mb][i];
+      v[i] = kSwiglu ? silu(x) * y : x;
+      v[4 + i] = y;
+    }
+    const int n = n0 + (kSwiglu ? 4 : 8) * g;
+    if (n < a.NO) store_few<kSwiglu ? 4 : 8>(a.out + (long long)(u.r0 + row) * a.NO + n, a.NO - n, v);
   }
 }
 
@@ -442,17 +777,40 @@ int check_rows(const void* wide, size_t wide_align, const void* codes, const voi
   return MOE_OK;
 }
 
+// Workgroups that take several tiles: as many as are resident at once, in eight
+// equal shares (one of each XCD), and not more than there can be tiles.
+constexpr int kCus = 256;
 template <class C>
 int launch_product(MxArgs a, bool swiglu, hipStream_t s) {
   const int bno = swiglu ? C::BN / 2 : C::BN;
   a.NT = (a.NO + bno - 1) / bno;
-  // the most tiles that `rows` rows in at most min(E, rows) experts make, in eight equal shares
+  const long long n = a.E < a.rows ? a.E : a.rows;
+  const long long most = (((a.rows - n) / C::BM + n) * a.NT + 7) / 8 * 8;
+  if (most > INT32_MAX / 2) return MOE_ERR_UNSUPPORTED;
+  const unsigned grid = (unsigned)(most < C::R * kCus ? most : C::R * kCus);
+  if (swiglu) mx4_product_kernel<C, true><<<grid, C::kThr, 0, s>>>(a);
+  else mx4_product_kernel<C, false><<<grid, C::kThr, 0, s>>>(a);
+  return done();
+}
+
+template <class C>
+int launch_thin(MxArgs a, bool swiglu, hipStream_t s) {
+  const int bno = swiglu ? C::BN / 2 : C::BN;
+  a.NT = (a.NO + bno - 1) / bno;
   const long long n = a.E < a.rows ? a.E : a.rows;
   const long long grid = (((a.rows - n) / C::BM + n) * a.NT + 7) / 8 * 8;
   if (grid * C::kThr >= 1ll << 32) return MOE_ERR_UNSUPPORTED;
-  if (swiglu) mx4_product_kernel<C, true><<<(unsigned)grid, C::kThr, 0, s>>>(a);
-  else mx4_product_kernel<C, false><<<(unsigned)grid, C::kThr, 0, s>>>(a);
+  if (swiglu) mx4_thin_kernel<C, true><<<(unsigned)grid, C::kThr, 0, s>>>(a);
+  else mx4_thin_kernel<C, false><<<(unsigned)grid, C::kThr, 0, s>>>(a);
   return done();
+}
+
+int route(const MxArgs& a, bool swiglu, hipStream_t s) {
+  const long long mean = a.rows / a.E;
+  if (mean <= 8 && a.KB <= 32) return launch_thin<MxThin<1, 8, 1>>(a, swiglu, s);
+  if (mean <= 8) return launch_thin<MxThin<1, 16, 1>>(a, swiglu, s);
+  if (mean >= 128) return launch_product<MxTile<256, 256, 2, 4, 4, 1>>(a, swiglu, s);
+  return launch_product<MxTile<64, 128, 1, 2, 4, 2>>(a, swiglu, s);
 }
 
 }  // namespace
@@ -515,13 +873,14 @@ extern "C" int moe_mx4_product(const void* a_codes, const void* a_scales, const 
                                void* stream) {
   if (a_rows < 0 || rows < 0 || K < 1 || N < 1 || E < 1 || (swiglu && N % 2)) return MOE_ERR_INVALID_ARG;
   const long long pitch = ((long long)K + kBlock - 1) / kBlock * kBlockBytes;
-  if (E > 1024 || rows > INT32_MAX || pitch * N > INT32_MAX || (a_rows > 0 && pitch > INT32_MAX / a_rows))
+  if (E > kMaxExperts || rows > INT32_MAX || pitch * N > INT32_MAX || (a_rows > 0 && pitch > INT32_MAX / a_rows))
     return MOE_ERR_UNSUPPORTED;
   if (rows > 0 && (!a_codes || !a_scales || !w_codes || !w_scales || !expert_offsets || !out)) return MOE_ERR_INVALID_ARG;
   if (!aligned(a_codes, 16) || !aligned(w_codes, 16) || !aligned(a_scales, 4) || !aligned(w_scales, 4) ||
       !aligned(expert_offsets, 4) || !aligned(row_ids, 4) || !aligned(out, 2) || !aligned(workspace, 256))
     return MOE_ERR_ALIGNMENT;
   if (rows == 0) return MOE_OK;
+  if (a_rows == 0) return MOE_ERR_INVALID_ARG;
   MxArgs a = {};
   a.a = (const uint8_t*)a_codes;
   a.as = (const uint8_t*)a_scales;
@@ -540,7 +899,5 @@ extern "C" int moe_mx4_product(const void* a_codes, const void* a_scales, const 
   a.KS = scale_pitch(K);
   a.NO = swiglu ? N / 2 : N;
   const hipStream_t s = (hipStream_t)stream;
-  const long long mean = rows / E;
-  if (mean >= 128) return launch_product<MxTile<256, 256, 2, 4, 3>>(a, swiglu, s);
-  return launch_product<MxTile<64, 128, 1, 2, 3>>(a, swiglu, s);
+  return route(a, swiglu != 0, s);
 }
