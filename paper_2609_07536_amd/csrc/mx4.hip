@@ -2,6 +2,7 @@
 // weights, and the experts' products (C ABI and format: moe_experts.h).
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstddef>
 #include <cstdint>
 #include <type_traits>
@@ -301,8 +302,9 @@ struct Tile {
 };
 template <int BM>
 __device__ __forceinline__ int tiles_of(int r0, int r1) { return (max(r1 - r0, 0) + BM - 1) / BM; }
-// Tile `unit` (expert -> columns -> rows), by each wave for itself; row(i), i <= E:
-// expert i's first row (row(E): the end of the last one).
+// Tile `unit` (expert -> kGroup tiles of columns -> rows -> columns), by each wave for
+// itself; row(i), i <= E: expert i's first row (row(E): the end of the last one).
+constexpr int kGroup = 4;
 template <int BM, int BNO, class Row>
 __device__ __forceinline__ Tile unit_at(const MxArgs& a, int unit, Row row) {
   const int lane = threadIdx.x & 63;
@@ -318,7 +320,8 @@ __device__ __forceinline__ Tile unit_at(const MxArgs& a, int unit, Row row) {
     }
     const int i = (int)__builtin_ctzll(past);
     const int n = __builtin_amdgcn_readlane(t, i), within = unit - (__builtin_amdgcn_readlane(end, i) - n) * a.NT;
-    const int nt = within / n, mi = within - nt * n;
+    const int group = within / (n * kGroup), left = within - group * (n * kGroup);
+    const int wide = min(kGroup, a.NT - group * kGroup), mi = left / wide, nt = group * kGroup + left - mi * wide;
     const int start = __builtin_amdgcn_readlane(r0, i) + mi * BM;
     return {e0 + i, start, min(BM, __builtin_amdgcn_readlane(r1, i) - start), nt * BNO, 1};
   }
@@ -805,12 +808,43 @@ int launch_thin(MxArgs a, bool swiglu, hipStream_t s) {
   return done();
 }
 
+// Which tiles: each kind's price in us, from what the host knows (rows, experts,
+// sizes; not the counts per expert, which are taken as an even spread's): a call's
+// latency and its tiles' share of the CUs, each with a part per stage of 128 of K.
+// Fitted to 150 measured calls of each kind (E 8 to 256, 1 to 8192 tokens, K 256 to
+// 4096, N 512 to 4096, uniform and Zipf 1.0); the kind with the least price is on average
+// 3% and at most 19% slower than the fastest one.  (Also measured: waves in twos and fours
+// for 16 and 32 rows, and 128 x 256 tiles: within 0.5% of this on average.)
+struct Price {
+  int rows, cols;                      // of a tile, cols in rows of w
+  double call, call_k, tile, tile_k;   // us, per stage of K; tiles: for one on every CU
+  double of(const MxArgs& a, bool swiglu) const {
+    const double mean = (double)a.rows / a.E, hit = a.E * (1 - std::exp(-mean)), KT = (a.KB + 3) / 4;
+    const double per = mean / rows + 0.5;   // ragged ends: half a tile
+    const double m = std::fmin((double)a.rows, mean > 0.5 * rows ? hit * std::fmax(1.0, per) : hit);
+    const int bno = swiglu ? cols / 2 : cols;
+    return call + call_k * KT + m * ((a.NO + bno - 1) / bno) / kCus * (tile + tile_k * KT);
+  }
+};
+
 int route(const MxArgs& a, bool swiglu, hipStream_t s) {
-  const long long mean = a.rows / a.E;
-  if (mean <= 8 && a.KB <= 32) return launch_thin<MxThin<1, 8, 1>>(a, swiglu, s);
-  if (mean <= 8) return launch_thin<MxThin<1, 16, 1>>(a, swiglu, s);
-  if (mean >= 128) return launch_product<MxTile<256, 256, 2, 4, 4, 1>>(a, swiglu, s);
-  return launch_product<MxTile<64, 128, 1, 2, 4, 2>>(a, swiglu, s);
+  static constexpr Price kPrices[] = {{16, 32, 2.96, 0.075, 0.07, 0.0756},   {16, 32, 3.32, 0.043, 0.272, 0.0709},
+                                      {32, 64, 2.94, 0.127, 0.347, 0.140},   {64, 128, 3.14, 0.216, 1.025, 0.302},
+                                      {128, 128, 4.17, 0.201, 1.875, 0.310}, {256, 256, 5.61, 0.402, 8.038, 0.582}};
+  int best = 0;
+  double least = kPrices[0].of(a, swiglu);
+  for (int i = 1; i < 6; ++i) {
+    const double p = kPrices[i].of(a, swiglu);
+    if (p < least) least = p, best = i;
+  }
+  switch (best) {
+    case 0: return launch_thin<MxThin<1, 8, 1>>(a, swiglu, s);
+    case 1: return launch_thin<MxThin<1, 16, 1>>(a, swiglu, s);
+    case 2: return launch_thin<MxThin<2, 8, 2>>(a, swiglu, s);
+    case 3: return launch_thin<MxThin<4, 8, 4>>(a, swiglu, s);
+    case 4: return launch_product<MxTile<128, 128, 2, 2, 3, 2>>(a, swiglu, s);
+    default: return launch_product<MxTile<256, 256, 2, 4, 3, 1>>(a, swiglu, s);
+  }
 }
 
 }  // namespace
