@@ -30,8 +30,13 @@ constexpr int kMaxExperts = 1024;
 constexpr int kOneLaunch = 4096;
 constexpr int kOneThreads = 1024;
 constexpr int kPlaceThreads = 256;
-constexpr int kChunk = 2048;          // slots, times what keeps the chunks at most kMaxChunks
+// Slots of a chunk: as few as spread the work over many CUs, while what every
+// workgroup adds up (chunks times experts) stays small.  Measured (us, 512 / 1024 /
+// 2048 slots): 98304 slots of 32 experts 8.9 / 10.2 / 12.3, 262144 of 64 15.2 / 12.5 /
+// 13.0, 131072 of 256 20.8 / 15.9 / 15.2, 65536 of 1024 38 / 27 / 23.
+constexpr int kLeastChunk = 512, kChunk = 2048;   // (past kChunk: times what keeps them at most kMaxChunks)
 constexpr int kMaxChunks = 256;
+constexpr long long kMaxCounts = 16384;
 
 struct SortArgs {
   const int32_t* ids;
@@ -42,13 +47,25 @@ struct SortArgs {
   int32_t* slot_rows;
   uint32_t* counts;      // [chunks][E], two launches only
   int slots, topk, E, first, id_bits;
-  int chunk, chunks;     // slots of a chunk (a multiple of kChunk)
+  int chunk, chunks;     // slots of a chunk (a multiple of 512)
 };
 
-// expert of slot s, or -1
-__device__ __forceinline__ int expert_of(const SortArgs& a, int s) {
-  const int64_t e = (int64_t)a.ids[s] - a.first;
+// the expert of an id, or -1
+__device__ __forceinline__ int expert_of(const SortArgs& a, int id) {
+  const int64_t e = (int64_t)id - a.first;
   return e >= 0 && e < a.E ? (int)e : -1;
+}
+
+// A wave's rounds of 64 slots, R of them by loads that are in flight together (one
+// after the other they took 8 of a large batch's 13 us).
+constexpr int kRounds = 8;
+// (end: of the wave's slots; lanes past it load the last one again)
+template <int R, class T>
+__device__ __forceinline__ void load_rounds(const T* p, int s, int end, T (&v)[R]) {
+  const int first = s - (int)(threadIdx.x & 63);
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    if (first + 64 * r < end) v[r] = p[min(s + 64 * r, end - 1)];
 }
 
 // the lanes that hold the same e (0 <= e < 2^bits) as this one, among `live`
@@ -66,9 +83,16 @@ __global__ void __launch_bounds__(kPlaceThreads) sort_count_kernel(SortArgs a) {
   for (int e = threadIdx.x; e < a.E; e += kPlaceThreads) n[e] = 0;
   __syncthreads();
   const int s0 = blockIdx.x * a.chunk, s1 = min(s0 + a.chunk, a.slots);
-  for (int s = s0 + (int)threadIdx.x; s < s1; s += kPlaceThreads) {
-    const int e = expert_of(a, s);
-    if (e >= 0) atomicAdd(&n[e], 1u);
+  const int wave = threadIdx.x >> 6, per = a.chunk / (kPlaceThreads / 64);
+  const int w1 = min(s0 + (wave + 1) * per, s1);
+  for (int s = s0 + wave * per + (int)(threadIdx.x & 63); s - (int)(threadIdx.x & 63) < w1; s += 64 * kRounds) {
+    int id[kRounds];
+    load_rounds<kRounds>(a.ids, s, w1, id);
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+      const int e = s + 64 * r < w1 ? expert_of(a, id[r]) : -1;
+      if (e >= 0) atomicAdd(&n[e], 1u);
+    }
   }
   __syncthreads();
   for (int e = threadIdx.x; e < a.E; e += kPlaceThreads)
@@ -102,9 +126,15 @@ __global__ void __launch_bounds__(kMaxThreads) sort_place_kernel(SortArgs a) {
   const int per = (a.chunk / 64 + waves - 1) / waves * 64;
   const int w0 = min(s0 + wave * per, s1), w1 = min(w0 + per, s1);
   uint32_t* mine = part + wave * a.E;
-  for (int s = w0 + lane; s < w1; s += 64) {
-    const int e = expert_of(a, s);
-    if (e >= 0) atomicAdd(&mine[e], 1u);
+  constexpr int R = kOne ? kRounds / 2 : kRounds;   // (a single workgroup has at most as many)
+  for (int s = w0 + lane; s - lane < w1; s += 64 * R) {
+    int id[R];
+    load_rounds<R>(a.ids, s, w1, id);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int e = s + 64 * r < w1 ? expert_of(a, id[r]) : -1;
+      if (e >= 0) atomicAdd(&mine[e], 1u);
+    }
   }
   if (!kOne) {
     // a thread adds up one expert's counts over every groups-th chunk
@@ -112,7 +142,7 @@ __global__ void __launch_bounds__(kMaxThreads) sort_place_kernel(SortArgs a) {
     for (int i = tid; i < groups * a.E; i += threads) {
       const int e = i % a.E;
       uint32_t n = 0, b = 0;
-#pragma unroll 4
+#pragma unroll 8
       for (int c = i / a.E; c < a.chunks; c += groups) {
         const uint32_t v = a.counts[(size_t)c * a.E + e];
         n += v;
@@ -160,25 +190,35 @@ __global__ void __launch_bounds__(kMaxThreads) sort_place_kernel(SortArgs a) {
   }
   __syncthreads();
   const int rows = (int)live;
-  for (int s = w0 + lane; s - lane < w1; s += 64) {
-    const int e = s < w1 ? expert_of(a, s) : -1;
-    const uint64_t same = same_expert(e, __ballot(e >= 0), a.id_bits);
-    if (s >= w1) continue;   // (lanes past the end: the last round)
-    int row = -1;
-    if (e >= 0) {
-      const uint32_t at = lds_get(&mine[e]);
-      const uint64_t lower = same & ((1ull << lane) - 1);
-      row = (int)at + __popcll(lower);
-      __builtin_amdgcn_wave_barrier();
-      if (lower == 0) lds_put(&mine[e], at + __popcll(same));
-      __builtin_amdgcn_wave_barrier();
-      a.token_ids[row] = s / a.topk;
-      a.gate_w[row] = a.gates[s];
-    }
-    a.slot_rows[s] = row;
-    if (s >= rows) {   // past the last row
-      a.token_ids[s] = -1;
-      a.gate_w[s] = 0.f;
+  for (int s0r = w0 + lane; s0r - lane < w1; s0r += 64 * R) {
+    int id[R];
+    float gate[R];
+    load_rounds<R>(a.ids, s0r, w1, id);
+    load_rounds<R>(a.gates, s0r, w1, gate);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int s = s0r + 64 * r;
+      if (s - lane >= w1) break;   // (uniform)
+      const int e = s < w1 ? expert_of(a, id[r]) : -1;
+      const uint64_t same = same_expert(e, __ballot(e >= 0), a.id_bits);
+      int row = -1;
+      if (e >= 0) {
+        const uint32_t at = lds_get(&mine[e]);
+        const uint64_t lower = same & ((1ull << lane) - 1);
+        row = (int)at + __popcll(lower);
+        __builtin_amdgcn_wave_barrier();
+        if (lower == 0) lds_put(&mine[e], at + __popcll(same));
+        __builtin_amdgcn_wave_barrier();
+        a.token_ids[row] = s / a.topk;
+        a.gate_w[row] = gate[r];
+      }
+      if (s < w1) {
+        a.slot_rows[s] = row;
+        if (s >= rows) {   // past the last row
+          a.token_ids[s] = -1;
+          a.gate_w[s] = 0.f;
+        }
+      }
     }
   }
 }
@@ -406,6 +446,11 @@ bool sort_plan(int32_t T, int32_t topk, int32_t E, SortPlan* p) {
   if (p->slots > INT32_MAX - (1 << 24)) return false;   // (indices past the last chunk stay below 2^31)
   const long long spread = (long long)kChunk * kMaxChunks;
   p->chunk = kChunk * (int)((p->slots + spread - 1) / spread);
+  for (int c = kLeastChunk; c < kChunk; c *= 2)
+    if ((p->slots + c - 1) / c * E <= kMaxCounts) {
+      p->chunk = c;
+      break;
+    }
   if (p->slots <= kOneLaunch) p->chunk = kOneLaunch;
   p->chunks = p->slots <= kOneLaunch ? 1 : (int)((p->slots + p->chunk - 1) / p->chunk);
   return true;

@@ -148,6 +148,14 @@ __global__ void __launch_bounds__(256) mx4_quantize_weights_kernel(const T* w, u
   for (int p = 0; p < 2; ++p) {
     const int b = wave + 4 * p, k0 = (b0 + b) * kBlock;
     float v[2][kBlock];
+    if (k0 + kBlock <= K && n0 + kWCols <= N) {   // a whole block of whole columns: no load waits for a test
+#pragma unroll
+      for (int k = 0; k < kBlock; ++k) {
+        const auto x = *(const typename Mem<T, 2>::type*)(src + (long long)(k0 + k) * N);
+        v[0][k] = (float)x[0];
+        v[1][k] = (float)x[1];
+      }
+    } else
 #pragma unroll
     for (int k = 0; k < kBlock; ++k) {
       v[0][k] = v[1][k] = 0.f;

@@ -14,8 +14,8 @@ from typing import NamedTuple, Optional
 
 import torch
 
-from .binding import MoeError, Workspace, _stream
-from .binding import lib as _base_lib
+from . import binding as _b
+from .binding import MoeError, Workspace
 
 EXPORTED = (
     "moe_sort_scratch_size", "moe_sort_by_expert", "moe_dispatch_rows", "moe_dispatch_rows_grad",
@@ -31,7 +31,7 @@ def lib() -> ctypes.CDLL:
     """The HIP library with this module's functions declared."""
     global _lib
     if _lib is None:
-        L = _base_lib()
+        L = _b.lib()
         vp, sz, i32, i64 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32, ctypes.c_int64
         L.moe_sort_scratch_size.argtypes = [i32, i32, i32]
         L.moe_sort_scratch_size.restype = sz
@@ -51,10 +51,34 @@ def lib() -> ctypes.CDLL:
     return _lib
 
 
-def _check(t, what, shape, *dtypes):
-    if t.dtype not in dtypes or t.shape != shape or not t.is_cuda or not t.is_contiguous():
-        raise TypeError(f"{what}: expected a contiguous CUDA tensor of {' or '.join(map(str, dtypes))} and shape "
-                        f"{tuple(shape)}, got {t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
+_BF16, _F32, _I32, _U8 = (torch.bfloat16,), (torch.float32,), (torch.int32,), (torch.uint8,)
+_FLOAT = (torch.bfloat16, torch.float32)
+
+
+def _check(t, what, shape, dtypes):
+    if t.dtype in dtypes and t.shape == shape and t.is_cuda and t.is_contiguous():
+        return
+    raise TypeError(f"{what}: expected a contiguous CUDA tensor of {' or '.join(map(str, dtypes))} and shape "
+                    f"{tuple(shape)}, got {t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
+
+
+def _two(t, what, dtypes):
+    """The shape of a matrix."""
+    shape = t.shape
+    if len(shape) == 2 and t.dtype in dtypes and t.is_cuda and t.is_contiguous():
+        return shape
+    raise TypeError(f"{what}: expected a contiguous CUDA matrix of {' or '.join(map(str, dtypes))}, got {t.dtype} "
+                    f"{tuple(shape)} on {t.device}, strides {t.stride()}")
+
+
+def _stream(stream):
+    """The handle of `stream`, or of the current one (by torch's raw accessors, as
+    in ``binding``; an int, which a call converts faster than a c_void_p)."""
+    if stream is not None:
+        return stream.cuda_stream
+    if _b._raw_stream is None or not torch.cuda.is_initialized():
+        return torch.cuda.current_stream().cuda_stream
+    return _b._raw_stream(_b._raw_device())
 
 
 def _empty(shape, dtype, device, stream):
@@ -64,20 +88,6 @@ def _empty(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
         return torch.empty(shape, dtype=dtype, device=device)
-
-
-def _output(out, what, shape, device, stream, *dtypes):
-    if out is None:
-        return _empty(shape, dtypes[0], device, stream)
-    _check(out, what, shape, *dtypes)
-    return out
-
-
-def _two(t, what, *dtypes):
-    if t.dim() != 2:
-        raise TypeError(f"{what}: expected two dimensions, got {tuple(t.shape)}")
-    _check(t, what, t.shape, *dtypes)
-    return t.shape
 
 
 def _done(r, what):
@@ -105,26 +115,30 @@ def sort_by_expert(expert_ids, gates, E: int, first_expert: int = 0, out: Option
     """moe_sort_by_expert: expert_ids int32 and gates fp32 [T, topk] to a Routing
     (a stable sort by expert).  Ids outside [first_expert, first_expert + E)
     are slots without a row.  scratch: uint8, at least sort_scratch_size bytes."""
-    T, topk = shape = _two(expert_ids, "expert_ids", torch.int32)
-    _check(gates, "gates", shape, torch.float32)
-    L, n, dev = lib(), T * topk, expert_ids.device
+    T, topk = shape = _two(expert_ids, "expert_ids", _I32)
+    _check(gates, "gates", shape, _F32)
+    n = T * topk
     if out is None:
+        dev = expert_ids.device
         out = Routing(_empty((E + 1,), torch.int32, dev, stream), _empty((n,), torch.int32, dev, stream),
                       _empty((n,), torch.float32, dev, stream), _empty(shape, torch.int32, dev, stream))
-    else:
-        _check(out.expert_offsets, "expert_offsets", (E + 1,), torch.int32)
-        _check(out.token_ids, "token_ids", (n,), torch.int32)
-        _check(out.gate_w, "gate_w", (n,), torch.float32)
-        _check(out.slot_rows, "slot_rows", shape, torch.int32)
-    need = L.moe_sort_scratch_size(T, topk, E) if n > 4096 else 0
-    if need and scratch is None:
-        scratch = _empty((need,), torch.uint8, dev, stream)
-    elif need:
-        _check(scratch, "scratch", scratch.shape, torch.uint8)
-    _done(L.moe_sort_by_expert(expert_ids.data_ptr(), gates.data_ptr(), out.expert_offsets.data_ptr(),
-                               out.token_ids.data_ptr(), out.gate_w.data_ptr(), out.slot_rows.data_ptr(),
-                               T, topk, E, first_expert, scratch.data_ptr() if need else None,
-                               scratch.numel() if need else 0, _stream(stream)), "moe_sort_by_expert")
+    offsets, token_ids, gate_w, slot_rows = out
+    _check(offsets, "expert_offsets", (E + 1,), _I32)
+    _check(token_ids, "token_ids", (n,), _I32)
+    _check(gate_w, "gate_w", (n,), _F32)
+    _check(slot_rows, "slot_rows", shape, _I32)
+    L, room = lib(), 0
+    if n > 4096:   # (the least that needs scratch)
+        room = L.moe_sort_scratch_size(T, topk, E)
+        if scratch is None:
+            scratch = _empty((room,), torch.uint8, expert_ids.device, stream)
+        _check(scratch, "scratch", scratch.shape, _U8)
+        room = scratch.numel()
+    r = L.moe_sort_by_expert(expert_ids.data_ptr(), gates.data_ptr(), offsets.data_ptr(), token_ids.data_ptr(),
+                             gate_w.data_ptr(), slot_rows.data_ptr(), T, topk, E, first_expert,
+                             scratch.data_ptr() if room else None, room, _stream(stream))
+    if r < 0:
+        raise MoeError(r, "moe_sort_by_expert")
     return out
 
 
@@ -135,29 +149,35 @@ def sort_scratch_size(T: int, topk: int, E: int) -> int:
 def dispatch_rows(x, slot_rows, rows: int, out=None, workspace: Optional[Workspace] = None, stream=None):
     """moe_dispatch_rows: x [T, H] of any type to [rows, H], each token's row
     copied to the rows of its slots.  Rows that no slot has are not written."""
-    T, topk = _two(slot_rows, "slot_rows", torch.int32)
-    _two(x, "x", x.dtype)
-    H = x.shape[1]
-    _check(x, "x", (T, H), x.dtype)
-    out = _output(out, "out", (rows, H), x.device, stream, x.dtype)
-    _done(lib().moe_dispatch_rows(x.data_ptr(), slot_rows.data_ptr(), out.data_ptr(), T, topk, rows,
-                                  H * x.element_size(), _status_word(workspace), _stream(stream)),
-          "moe_dispatch_rows")
+    T, topk = _two(slot_rows, "slot_rows", _I32)
+    dtypes = (x.dtype,)
+    H = _two(x, "x", dtypes)[1]
+    if x.shape[0] != T:
+        raise TypeError(f"x: {x.shape[0]} rows, slot_rows {T}")
+    if out is None:
+        out = _empty((rows, H), x.dtype, x.device, stream)
+    else:
+        _check(out, "out", (rows, H), dtypes)
+    r = lib().moe_dispatch_rows(x.data_ptr(), slot_rows.data_ptr(), out.data_ptr(), T, topk, rows,
+                                H * x.element_size(), _status_word(workspace), _stream(stream))
+    if r < 0:
+        raise MoeError(r, "moe_dispatch_rows")
     return out
 
 
 def dispatch_rows_grad(d, slot_rows, out=None, workspace: Optional[Workspace] = None, stream=None):
     """moe_dispatch_rows_grad: d [rows, H] (bf16 or fp32) to dx [T, H] (of d's type,
     or `out`'s): the sum of each token's rows, in fp32, rounded once."""
-    T, topk = _two(slot_rows, "slot_rows", torch.int32)
-    rows, H = _two(d, "d", torch.bfloat16, torch.float32)
+    T, topk = _two(slot_rows, "slot_rows", _I32)
+    rows, H = _two(d, "d", _FLOAT)
     if out is None:
         out = _empty((T, H), d.dtype, d.device, stream)
     else:
-        _check(out, "out", (T, H), torch.bfloat16, torch.float32)
-    _done(lib().moe_dispatch_rows_grad(d.data_ptr(), slot_rows.data_ptr(), out.data_ptr(), T, topk, rows, H,
-                                       _TYPES[d.dtype], _TYPES[out.dtype], _status_word(workspace),
-                                       _stream(stream)), "moe_dispatch_rows_grad")
+        _check(out, "out", (T, H), _FLOAT)
+    r = lib().moe_dispatch_rows_grad(d.data_ptr(), slot_rows.data_ptr(), out.data_ptr(), T, topk, rows, H,
+                                     _TYPES[d.dtype], _TYPES[out.dtype], _status_word(workspace), _stream(stream))
+    if r < 0:
+        raise MoeError(r, "moe_dispatch_rows_grad")
     return out
 
 
@@ -166,35 +186,39 @@ def combine_rows(y, slot_rows, gates, out=None, dtype=torch.float32, workspace: 
     """moe_combine_rows: y [rows, H] (bf16 or fp32) to out [T, H] (`dtype`: fp32 or
     bf16): the sum of each token's rows weighted by gates fp32 [T, topk], in
     fp32, rounded once."""
-    T, topk = shape = _two(slot_rows, "slot_rows", torch.int32)
-    _check(gates, "gates", shape, torch.float32)
-    rows, H = _two(y, "y", torch.bfloat16, torch.float32)
+    T, topk = shape = _two(slot_rows, "slot_rows", _I32)
+    _check(gates, "gates", shape, _F32)
+    rows, H = _two(y, "y", _FLOAT)
     if out is None:
         out = _empty((T, H), dtype, y.device, stream)
-    _check(out, "out", (T, H), torch.bfloat16, torch.float32)
-    _done(lib().moe_combine_rows(y.data_ptr(), slot_rows.data_ptr(), gates.data_ptr(), out.data_ptr(), T, topk,
-                                 rows, H, _TYPES[y.dtype], _TYPES[out.dtype], _status_word(workspace),
-                                 _stream(stream)), "moe_combine_rows")
+    _check(out, "out", (T, H), _FLOAT)
+    r = lib().moe_combine_rows(y.data_ptr(), slot_rows.data_ptr(), gates.data_ptr(), out.data_ptr(), T, topk, rows,
+                               H, _TYPES[y.dtype], _TYPES[out.dtype], _status_word(workspace), _stream(stream))
+    if r < 0:
+        raise MoeError(r, "moe_combine_rows")
     return out
 
 
 def combine_rows_grad(d_out, y, slot_rows, gates, out=None, workspace: Optional[Workspace] = None, stream=None):
     """moe_combine_rows_grad: d_out [T, H] and y [rows, H] (each bf16 or fp32) to
     (dy [rows, H] of y's type, dgates fp32 [T, topk]); `out`: that pair."""
-    T, topk = shape = _two(slot_rows, "slot_rows", torch.int32)
-    _check(gates, "gates", shape, torch.float32)
-    rows, H = _two(y, "y", torch.bfloat16, torch.float32)
-    _check(d_out, "d_out", (T, H), torch.bfloat16, torch.float32)
+    T, topk = shape = _two(slot_rows, "slot_rows", _I32)
+    _check(gates, "gates", shape, _F32)
+    rows, H = _two(y, "y", _FLOAT)
+    _check(d_out, "d_out", (T, H), _FLOAT)
     if out is None:
-        out = (_empty((rows, H), y.dtype, y.device, stream), _empty(shape, torch.float32, y.device, stream))
+        dy = _empty((rows, H), y.dtype, y.device, stream)
+        dgates = _empty(shape, torch.float32, y.device, stream)
     else:
-        _check(out[0], "dy", (rows, H), y.dtype)
-        _check(out[1], "dgates", shape, torch.float32)
-    _done(lib().moe_combine_rows_grad(d_out.data_ptr(), y.data_ptr(), slot_rows.data_ptr(), gates.data_ptr(),
-                                      out[0].data_ptr(), out[1].data_ptr(), T, topk, rows, H,
-                                      _TYPES[d_out.dtype], _TYPES[y.dtype], _status_word(workspace),
-                                      _stream(stream)), "moe_combine_rows_grad")
-    return tuple(out)
+        dy, dgates = out
+        _check(dy, "dy", (rows, H), (y.dtype,))
+        _check(dgates, "dgates", shape, _F32)
+    r = lib().moe_combine_rows_grad(d_out.data_ptr(), y.data_ptr(), slot_rows.data_ptr(), gates.data_ptr(),
+                                    dy.data_ptr(), dgates.data_ptr(), T, topk, rows, H, _TYPES[d_out.dtype],
+                                    _TYPES[y.dtype], _status_word(workspace), _stream(stream))
+    if r < 0:
+        raise MoeError(r, "moe_combine_rows_grad")
+    return dy, dgates
 
 
 # ---- microscaled 4-bit floating point -----------------------------------------------
@@ -209,60 +233,67 @@ class MX4(NamedTuple):
 
 
 def _mx4_shapes(lead, K):
-    blocks = -(-K // 32)
-    return (*lead, 16 * blocks), (*lead, (blocks + 3) // 4 * 4)
-
-
-def _mx4_out(out, lead, K, device, stream):
-    codes, scales = _mx4_shapes(lead, K)
-    if out is None:
-        return MX4(_empty(codes, torch.uint8, device, stream), _empty(scales, torch.uint8, device, stream), K)
-    _mx4_check(out, "out", lead)
-    if out.K != K:
-        raise TypeError(f"out: K is {out.K}, expected {K}")
-    return out
+    blocks = (K + 31) >> 5
+    return (*lead, 16 * blocks), (*lead, (blocks + 3) & ~3)
 
 
 def _mx4_check(m, what, lead):
-    codes, scales = _mx4_shapes(lead, m.K)
-    _check(m.codes, what + ".codes", codes, torch.uint8)
-    _check(m.scales, what + ".scales", scales, torch.uint8)
+    codes, scales, K = m
+    code_shape, scale_shape = _mx4_shapes(lead, K)
+    _check(codes, what + ".codes", code_shape, _U8)
+    _check(scales, what + ".scales", scale_shape, _U8)
+
+
+def _mx4_out(out, lead, K, device, stream):
+    if out is None:
+        codes, scales = _mx4_shapes(lead, K)
+        return MX4(_empty(codes, torch.uint8, device, stream), _empty(scales, torch.uint8, device, stream), K)
+    if out.K != K:
+        raise TypeError(f"out: K is {out.K}, expected {K}")
+    _mx4_check(out, "out", lead)
+    return out
 
 
 def mx4_quantize(x, out: Optional[MX4] = None, stream=None) -> MX4:
     """moe_mx4_quantize: x [..., K], bf16 or fp32."""
-    _check(x, "x", x.shape, torch.bfloat16, torch.float32)
-    if x.dim() < 1:
+    shape = x.shape
+    _check(x, "x", shape, _FLOAT)
+    if len(shape) < 1:
         raise TypeError("x: expected at least one dimension")
-    K, lead = x.shape[-1], x.shape[:-1]
+    K, lead = shape[-1], shape[:-1]
     out = _mx4_out(out, lead, K, x.device, stream)
-    _done(lib().moe_mx4_quantize(x.data_ptr(), out.codes.data_ptr(), out.scales.data_ptr(), lead.numel(), K,
-                                 _TYPES[x.dtype], _stream(stream)), "moe_mx4_quantize")
+    r = lib().moe_mx4_quantize(x.data_ptr(), out[0].data_ptr(), out[1].data_ptr(), lead.numel(), K,
+                               _TYPES[x.dtype], _stream(stream))
+    if r < 0:
+        raise MoeError(r, "moe_mx4_quantize")
     return out
 
 
 def mx4_quantize_weights(w, out: Optional[MX4] = None, stream=None) -> MX4:
     """moe_mx4_quantize_weights: w [E, K, N] (bf16 or fp32, the layout of w2 and of
     w_gate_up) to the MX4 [E, N, K] that mx4_product reads."""
-    _check(w, "w", w.shape, torch.bfloat16, torch.float32)
+    _check(w, "w", w.shape, _FLOAT)
     if w.dim() != 3:
         raise TypeError(f"w: expected [E, K, N], got {tuple(w.shape)}")
     E, K, N = w.shape
     out = _mx4_out(out, (E, N), K, w.device, stream)
-    _done(lib().moe_mx4_quantize_weights(w.data_ptr(), out.codes.data_ptr(), out.scales.data_ptr(), E, K, N,
+    _done(lib().moe_mx4_quantize_weights(w.data_ptr(), out[0].data_ptr(), out[1].data_ptr(), E, K, N,
                                          _TYPES[w.dtype], _stream(stream)), "moe_mx4_quantize_weights")
     return out
 
 
 def mx4_dequantize(m: MX4, out=None, dtype=torch.bfloat16, stream=None):
     """moe_mx4_dequantize: the values of `m` [..., K] as bf16 or fp32 (exact in both)."""
-    lead = m.codes.shape[:-1]
+    codes, scales, K = m
+    lead = codes.shape[:-1]
     _mx4_check(m, "m", lead)
     if out is None:
-        out = _empty((*lead, m.K), dtype, m.codes.device, stream)
-    _check(out, "out", (*lead, m.K), torch.bfloat16, torch.float32)
-    _done(lib().moe_mx4_dequantize(m.codes.data_ptr(), m.scales.data_ptr(), out.data_ptr(), lead.numel(), m.K,
-                                   _TYPES[out.dtype], _stream(stream)), "moe_mx4_dequantize")
+        out = _empty((*lead, K), dtype, codes.device, stream)
+    _check(out, "out", (*lead, K), _FLOAT)
+    r = lib().moe_mx4_dequantize(codes.data_ptr(), scales.data_ptr(), out.data_ptr(), lead.numel(), K,
+                                 _TYPES[out.dtype], _stream(stream))
+    if r < 0:
+        raise MoeError(r, "moe_mx4_dequantize")
     return out
 
 
@@ -271,20 +302,30 @@ def mx4_product(a: MX4, w: MX4, expert_offsets, rows: int, row_ids=None, swiglu:
     """moe_mx4_product: a [a_rows, K] and w [E, N, K] to bf16 [rows, N], or with
     swiglu [rows, N / 2]; row_ids int32 (at least `rows`): the row of `a` that
     each row takes.  Rows from expert_offsets[E] on are not written."""
-    if a.codes.dim() != 2 or w.codes.dim() != 3 or a.K != w.K:
-        raise TypeError(f"expected a [rows, K] and w [E, N, K], got {tuple(a.codes.shape)}, K = {a.K}, and "
-                        f"{tuple(w.codes.shape)}, K = {w.K}")
-    a_rows, (E, N) = a.codes.shape[0], w.codes.shape[:2]
+    a_codes, a_scales, K = a
+    w_codes, w_scales, _ = w
+    a_shape, w_shape = a_codes.shape, w_codes.shape
+    if len(a_shape) != 2 or len(w_shape) != 3 or K != w.K:
+        raise TypeError(f"expected a [rows, K] and w [E, N, K], got {tuple(a_shape)}, K = {K}, and "
+                        f"{tuple(w_shape)}, K = {w.K}")
+    a_rows, E, N = a_shape[0], w_shape[0], w_shape[1]
     _mx4_check(a, "a", (a_rows,))
     _mx4_check(w, "w", (E, N))
-    _check(expert_offsets, "expert_offsets", (E + 1,), torch.int32)
+    _check(expert_offsets, "expert_offsets", (E + 1,), _I32)
     if row_ids is not None:
-        _check(row_ids, "row_ids", row_ids.shape, torch.int32)
-    if rows > (row_ids.numel() if row_ids is not None else a_rows):
-        raise TypeError(f"{rows} rows of {a_rows}" + (f", {row_ids.numel()} row_ids" if row_ids is not None else ""))
-    out = _output(out, "out", (rows, N // 2 if swiglu else N), a.codes.device, stream, torch.bfloat16)
-    _done(lib().moe_mx4_product(a.codes.data_ptr(), a.scales.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr(),
-                                expert_offsets.data_ptr(), row_ids.data_ptr() if row_ids is not None else None,
-                                out.data_ptr(), a_rows, rows, a.K, N, E, int(swiglu), _status_word(workspace),
-                                _stream(stream)), "moe_mx4_product")
+        _check(row_ids, "row_ids", row_ids.shape, _I32)
+    have = a_rows if row_ids is None else row_ids.numel()
+    if rows > have:
+        raise TypeError(f"{rows} rows, but {have} " + ("of a" if row_ids is None else "row_ids"))
+    shape = (rows, N // 2 if swiglu else N)
+    if out is None:
+        out = _empty(shape, torch.bfloat16, a_codes.device, stream)
+    else:
+        _check(out, "out", shape, _BF16)
+    r = lib().moe_mx4_product(a_codes.data_ptr(), a_scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(),
+                              expert_offsets.data_ptr(), None if row_ids is None else row_ids.data_ptr(),
+                              out.data_ptr(), a_rows, rows, K, N, E, swiglu, _status_word(workspace),
+                              _stream(stream))
+    if r < 0:
+        raise MoeError(r, "moe_mx4_product")
     return out
