@@ -143,6 +143,30 @@ int moe_mx4_product(const void* a_codes, const void* a_scales, const void* w_cod
                     void* out, int64_t a_rows, int64_t rows, int32_t K, int32_t N, int32_t E,
                     int32_t swiglu, void* workspace, void* stream);
 
+/* Bytes of scratch moe_mx4_layer_forward needs (0 for invalid arguments); its
+ * contents do not matter, before or after. */
+size_t moe_mx4_layer_scratch_size(int32_t T, int32_t H, int32_t I, int32_t topk);
+
+/* The post-router layer with its experts in 4 bits, as five launches on stream:
+ * hidden quantised; the up-projection with the token gather and SwiGLU; its
+ * outputs (bf16) quantised; the down-projection (bf16); the combine.
+ *   hidden          device bf16 [T, H]
+ *   w1              mx4 [E, 2 I, H]: an expert's I gate rows, then its I up rows
+ *   w2              mx4 [E, H, I]
+ *   expert_offsets, token_ids, slot_rows
+ *                   as moe_sort_by_expert writes them (token_ids [T topk])
+ *   gates           device fp32 [T, topk]
+ *   out             device [T, H] of out_type, fully written
+ *   scratch         16-byte aligned, moe_mx4_layer_scratch_size bytes
+ *   workspace       NULL, or where bad entries are flagged
+ * Limits as for the functions it runs. */
+int moe_mx4_layer_forward(const void* hidden, const void* w1_codes, const void* w1_scales,
+                          const void* w2_codes, const void* w2_scales,
+                          const int32_t* expert_offsets, const int32_t* token_ids,
+                          const int32_t* slot_rows, const float* gates, void* out, int32_t T,
+                          int32_t H, int32_t I, int32_t E, int32_t topk, int32_t out_type,
+                          void* scratch, size_t scratch_bytes, void* workspace, void* stream);
+
 /* ABI version of this header (major * 100 + minor): 100. */
 int moe_experts_abi_version(void);
 

@@ -87,7 +87,7 @@ def mx4_values(codes, scales):
     v = np.where(codes >= 8, -1.0, 1.0) * GRID[codes % 8]
     v = v * np.exp2(scales.astype(np.float64) - 127)[..., None]
     v = np.where(scales[..., None] == 255, np.nan, v)
-    return v.reshape(v.shape[:-2] + (-1,))
+    return v.reshape(v.shape[:-2] + (v.shape[-2] * v.shape[-1],))
 
 
 def mx4_pack(codes, scales):

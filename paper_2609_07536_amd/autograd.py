@@ -1,0 +1,58 @@
+"""The rows' way to the experts and back as differentiable functions: their
+gradients are the library's own kernels (``experts``).
+
+    routing = experts.sort_by_expert(ids, gates, E)      # ids, gates [T, topk]
+    rows = autograd.dispatch(x, routing)                 # [T topk, H], by expert
+    ... the experts on rows offsets[e] .. offsets[e + 1] ...
+    out = autograd.combine(y, routing, gates)            # [T, H]
+
+The choice itself (the ids) has no gradient; the gates do, through combine.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import experts as X
+
+
+class _Dispatch(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, slot_rows):
+        ctx.save_for_backward(slot_rows)
+        # rows that no slot has are zeros, as their gradients are
+        out = torch.zeros((slot_rows.numel(), x.shape[1]), dtype=x.dtype, device=x.device)
+        return X.dispatch_rows(x.contiguous(), slot_rows, slot_rows.numel(), out=out)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d):
+        (slot_rows,) = ctx.saved_tensors
+        return X.dispatch_rows_grad(d.contiguous(), slot_rows), None
+
+
+class _Combine(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, y, slot_rows, gates, dtype):
+        y, gates = y.contiguous(), gates.contiguous()
+        ctx.save_for_backward(y, slot_rows, gates)
+        return X.combine_rows(y, slot_rows, gates, dtype=dtype)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d):
+        y, slot_rows, gates = ctx.saved_tensors
+        out = (torch.zeros_like(y), torch.empty_like(gates))
+        dy, dgates = X.combine_rows_grad(d.contiguous(), y, slot_rows, gates, out=out)
+        return dy, None, dgates, None
+
+
+def dispatch(x, routing: X.Routing):
+    """x [T, H] (bf16 or fp32) to [T topk, H]: each token's row at the rows of its
+    slots, zeros at rows that no slot has."""
+    return _Dispatch.apply(x, routing.slot_rows)
+
+
+def combine(y, routing: X.Routing, gates, dtype=torch.float32):
+    """y [T topk, H] (bf16 or fp32) to [T, H]: the sum of each token's rows weighted
+    by gates fp32 [T, topk]."""
+    return _Combine.apply(y, routing.slot_rows, gates, dtype)

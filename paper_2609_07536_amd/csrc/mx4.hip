@@ -943,3 +943,71 @@ extern "C" int moe_mx4_product(const void* a_codes, const void* a_scales, const 
   const hipStream_t s = (hipStream_t)stream;
   return route(a, swiglu != 0, s);
 }
+
+namespace {
+
+// The layer's scratch: activations in 4 bits and in bf16, each from a 256-byte line on.
+struct LayerScratch {
+  size_t hc, hs, x, xc, xs, y, bytes;
+};
+bool layer_scratch(int32_t T, int32_t H, int32_t I, int32_t topk, LayerScratch* l) {
+  if (T < 0 || H < 1 || I < 1 || topk < 1 || topk > 64 || H > INT32_MAX - 256 || I > INT32_MAX - 256) return false;
+  const size_t rows = (size_t)T * topk;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += (bytes + 255) / 256 * 256;
+    return here;
+  };
+  l->hc = take((size_t)T * blocks_of(H) * kBlockBytes);
+  l->hs = take((size_t)T * scale_pitch(H));
+  l->x = take(rows * I * 2);
+  l->xc = take(rows * blocks_of(I) * kBlockBytes);
+  l->xs = take(rows * scale_pitch(I));
+  l->y = take(rows * H * 2);
+  l->bytes = at;
+  return true;
+}
+
+}  // namespace
+
+extern "C" size_t moe_mx4_layer_scratch_size(int32_t T, int32_t H, int32_t I, int32_t topk) {
+  LayerScratch l;
+  return layer_scratch(T, H, I, topk, &l) ? l.bytes : 0;
+}
+
+extern "C" int moe_mx4_layer_forward(const void* hidden, const void* w1_codes, const void* w1_scales,
+                                     const void* w2_codes, const void* w2_scales, const int32_t* expert_offsets,
+                                     const int32_t* token_ids, const int32_t* slot_rows, const float* gates, void* out,
+                                     int32_t T, int32_t H, int32_t I, int32_t E, int32_t topk, int32_t out_type,
+                                     void* scratch, size_t scratch_bytes, void* workspace, void* stream) {
+  LayerScratch l;
+  if (T < 0 || H < 1 || I < 1 || E < 1 || topk < 1 || !type_ok(out_type)) return MOE_ERR_INVALID_ARG;
+  if (!layer_scratch(T, H, I, topk, &l) || I > INT32_MAX / 2 || (long long)T * topk > INT32_MAX) return MOE_ERR_UNSUPPORTED;
+  if (T == 0) return MOE_OK;
+  // (everything is looked at before the first launch)
+  if (!hidden || !w1_codes || !w1_scales || !w2_codes || !w2_scales || !expert_offsets || !token_ids || !slot_rows ||
+      !gates || !out)
+    return MOE_ERR_INVALID_ARG;
+  if (!scratch || scratch_bytes < l.bytes) return MOE_ERR_WORKSPACE;
+  if (!aligned(hidden, 2) || !aligned(w1_codes, 16) || !aligned(w1_scales, 4) || !aligned(w2_codes, 16) ||
+      !aligned(w2_scales, 4) || !aligned(expert_offsets, 4) || !aligned(token_ids, 4) || !aligned(slot_rows, 4) ||
+      !aligned(gates, 4) || !aligned(out, type_size(out_type)) || !aligned(scratch, 16) || !aligned(workspace, 256))
+    return MOE_ERR_ALIGNMENT;
+  const long long rows = (long long)T * topk, ph = (long long)blocks_of(H) * kBlockBytes,
+                  pi = (long long)blocks_of(I) * kBlockBytes;
+  if (E > kMaxExperts || ph * T > INT32_MAX || ph * 2 * I > INT32_MAX || pi * rows > INT32_MAX || pi * H > INT32_MAX)
+    return MOE_ERR_UNSUPPORTED;
+  uint8_t* s = (uint8_t*)scratch;
+  int r = moe_mx4_quantize(hidden, s + l.hc, s + l.hs, T, H, MOE_BF16, stream);
+  if (r == MOE_OK)
+    r = moe_mx4_product(s + l.hc, s + l.hs, w1_codes, w1_scales, expert_offsets, token_ids, s + l.x, T, rows, H, 2 * I,
+                        E, 1, workspace, stream);
+  if (r == MOE_OK) r = moe_mx4_quantize(s + l.x, s + l.xc, s + l.xs, rows, I, MOE_BF16, stream);
+  if (r == MOE_OK)
+    r = moe_mx4_product(s + l.xc, s + l.xs, w2_codes, w2_scales, expert_offsets, nullptr, s + l.y, rows, rows, I, H, E,
+                        0, workspace, stream);
+  if (r == MOE_OK)
+    r = moe_combine_rows(s + l.y, slot_rows, gates, out, T, topk, rows, H, MOE_BF16, out_type, workspace, stream);
+  return r;
+}

@@ -20,7 +20,8 @@ from .binding import MoeError, Workspace
 EXPORTED = (
     "moe_sort_scratch_size", "moe_sort_by_expert", "moe_dispatch_rows", "moe_dispatch_rows_grad",
     "moe_combine_rows", "moe_combine_rows_grad", "moe_mx4_quantize", "moe_mx4_quantize_weights",
-    "moe_mx4_dequantize", "moe_mx4_product", "moe_experts_abi_version",
+    "moe_mx4_dequantize", "moe_mx4_product", "moe_mx4_layer_scratch_size", "moe_mx4_layer_forward",
+    "moe_experts_abi_version",
 )
 
 _TYPES = {torch.bfloat16: 0, torch.float32: 1}   # moe_type_t
@@ -34,7 +35,6 @@ def lib() -> ctypes.CDLL:
         L = _b.lib()
         vp, sz, i32, i64 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32, ctypes.c_int64
         L.moe_sort_scratch_size.argtypes = [i32, i32, i32]
-        L.moe_sort_scratch_size.restype = sz
         L.moe_sort_by_expert.argtypes = [vp] * 6 + [i32] * 4 + [vp, sz, vp]
         L.moe_dispatch_rows.argtypes = [vp] * 3 + [i32, i32, i64, i64, vp, vp]
         L.moe_dispatch_rows_grad.argtypes = [vp] * 3 + [i32, i32, i64, i32, i32, i32, vp, vp]
@@ -44,9 +44,10 @@ def lib() -> ctypes.CDLL:
         L.moe_mx4_quantize_weights.argtypes = [vp] * 3 + [i32, i32, i32, i32, vp]
         L.moe_mx4_dequantize.argtypes = [vp] * 3 + [i64, i32, i32, vp]
         L.moe_mx4_product.argtypes = [vp] * 7 + [i64, i64, i32, i32, i32, i32, vp, vp]
+        L.moe_mx4_layer_scratch_size.argtypes = [i32] * 4
+        L.moe_mx4_layer_forward.argtypes = [vp] * 10 + [i32] * 6 + [vp, sz, vp, vp]
         for name in EXPORTED:
-            if name != "moe_sort_scratch_size":
-                getattr(L, name).restype = ctypes.c_int
+            getattr(L, name).restype = sz if name.endswith("_size") else ctypes.c_int
         _lib = L
     return _lib
 
@@ -328,4 +329,47 @@ def mx4_product(a: MX4, w: MX4, expert_offsets, rows: int, row_ids=None, swiglu:
                               _stream(stream))
     if r < 0:
         raise MoeError(r, "moe_mx4_product")
+    return out
+
+
+def mx4_layer_scratch_size(T: int, H: int, I: int, topk: int) -> int:
+    return int(lib().moe_mx4_layer_scratch_size(T, H, I, topk))
+
+
+def layer_forward_mx4(hidden, w1: MX4, w2: MX4, routing: Routing, gates, out=None, dtype=torch.float32,
+                      scratch=None, workspace: Optional[Workspace] = None, stream=None):
+    """moe_mx4_layer_forward, the post-router layer with its experts in 4 bits:
+    hidden bf16 [T, H]; w1 [E, 2I, H] and w2 [E, H, I] in MX4
+    (mx4_quantize_weights of w_gate_up [E, H, 2I] and w2 [E, I, H]); routing from
+    sort_by_expert of gates [T, topk]; returns out [T, H] (`dtype`: fp32 or bf16).
+    scratch: uint8, at least mx4_layer_scratch_size bytes (allocated if None)."""
+    T, H = _two(hidden, "hidden", _BF16)
+    if len(w1.codes.shape) != 3 or w1.codes.shape[1] % 2 or w1.K != H:
+        raise TypeError(f"w1: expected [E, 2I, {H}] in MX4, got {tuple(w1.codes.shape)}, K = {w1.K}")
+    E, I = w1.codes.shape[0], w1.codes.shape[1] // 2
+    _mx4_check(w1, "w1", (E, 2 * I))
+    if w2.K != I:
+        raise TypeError(f"w2: K is {w2.K}, expected {I}")
+    _mx4_check(w2, "w2", (E, H))
+    offsets, token_ids, _, slot_rows = routing
+    shape = _two(slot_rows, "slot_rows", _I32)
+    topk = shape[1]
+    if shape[0] != T:
+        raise TypeError(f"slot_rows: {shape[0]} tokens, hidden {T}")
+    _check(gates, "gates", shape, _F32)
+    _check(offsets, "expert_offsets", (E + 1,), _I32)
+    _check(token_ids, "token_ids", (T * topk,), _I32)
+    if out is None:
+        out = _empty((T, H), dtype, hidden.device, stream)
+    _check(out, "out", (T, H), _FLOAT)
+    L = lib()
+    if scratch is None:
+        scratch = _empty((L.moe_mx4_layer_scratch_size(T, H, I, topk),), torch.uint8, hidden.device, stream)
+    _check(scratch, "scratch", scratch.shape, _U8)
+    r = L.moe_mx4_layer_forward(hidden.data_ptr(), w1.codes.data_ptr(), w1.scales.data_ptr(), w2.codes.data_ptr(),
+                                w2.scales.data_ptr(), offsets.data_ptr(), token_ids.data_ptr(), slot_rows.data_ptr(),
+                                gates.data_ptr(), out.data_ptr(), T, H, I, E, topk, _TYPES[out.dtype],
+                                scratch.data_ptr(), scratch.numel(), _status_word(workspace), _stream(stream))
+    if r < 0:
+        raise MoeError(r, "moe_mx4_layer_forward")
     return out
