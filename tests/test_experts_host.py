@@ -83,3 +83,83 @@ def test_binding_refusals():
                  lambda: X.combine_rows_grad(x, x, ids, g)):
         with pytest.raises(TypeError):
             call()
+
+
+def _mx(name, a=P, b=P, c=P, rows=8, K=64, t=0, E=2, N=8):
+    L = X.lib()
+    if name == "weights":
+        return L.moe_mx4_quantize_weights(a, b, c, E, K, N, t, None)
+    if name == "quantize":
+        return L.moe_mx4_quantize(a, b, c, rows, K, t, None)
+    return L.moe_mx4_dequantize(b, c, a, rows, K, t, None)
+
+
+@pytest.mark.parametrize("name", ["quantize", "weights", "dequantize"])
+def test_mx4_refusals(name):
+    for bad in (dict(K=0), dict(t=2), dict(t=-1), dict(a=None), dict(b=None), dict(c=None)):
+        assert _mx(name, **bad) == B.MOE_ERR_INVALID_ARG, bad
+    for bad in (dict(K=2 ** 31 - 1), dict(K=2 ** 20, rows=2 ** 40, E=2 ** 15, N=2 ** 20)):
+        assert _mx(name, **bad) == B.MOE_ERR_UNSUPPORTED, bad
+    for bad in (dict(a=P + 1), dict(a=P + 2, t=1), dict(b=P + 8), dict(c=P + 2)):
+        assert _mx(name, **bad) == B.MOE_ERR_ALIGNMENT, bad
+    if name == "weights":
+        assert _mx(name, E=0) == _mx(name, N=0) == B.MOE_ERR_INVALID_ARG
+    else:
+        assert _mx(name, rows=-1) == B.MOE_ERR_INVALID_ARG
+        assert _mx(name, rows=0, a=None, b=None, c=None) == B.MOE_OK
+
+
+def _product(a=P, s=P, w=P, ws=P, off=P, ids=P, out=P, a_rows=8, rows=16, K=64, N=8, E=2, swiglu=0, work=None):
+    return X.lib().moe_mx4_product(a, s, w, ws, off, ids, out, a_rows, rows, K, N, E, swiglu, work, None)
+
+
+def test_product_refusals():
+    for bad in (dict(a=None), dict(s=None), dict(w=None), dict(ws=None), dict(off=None), dict(out=None), dict(a_rows=-1),
+                dict(rows=-1), dict(K=0), dict(N=0), dict(E=0), dict(N=9, swiglu=1), dict(a_rows=0)):
+        assert _product(**bad) == B.MOE_ERR_INVALID_ARG, bad
+    for bad in (dict(E=1025), dict(rows=2 ** 31), dict(a_rows=2 ** 31, K=32), dict(K=2 ** 20, N=2 ** 12)):
+        assert _product(**bad) == B.MOE_ERR_UNSUPPORTED, bad
+    for bad in (dict(a=P + 8), dict(s=P + 2), dict(w=P + 8), dict(ws=P + 1), dict(off=P + 2), dict(ids=P + 2),
+                dict(out=P + 1), dict(work=P + 128)):
+        assert _product(**bad) == B.MOE_ERR_ALIGNMENT, bad
+    assert _product(rows=0, a=None, s=None, w=None, ws=None, off=None, ids=None, out=None) == B.MOE_OK
+
+
+def _layer(h=P, w=P, off=P, rows_in=P, g=P, out=P, T=4, H=64, I=32, E=4, k=2, t=1, scratch=P, nbytes=1 << 30, ws=None):
+    return X.lib().moe_mx4_layer_forward(h, w, P, P, P, off, P, rows_in, g, out, T, H, I, E, k, t, scratch, nbytes, ws,
+                                         None)
+
+
+def test_layer_refusals():
+    for bad in (dict(h=None), dict(w=None), dict(off=None), dict(rows_in=None), dict(g=None), dict(out=None), dict(T=-1),
+                dict(H=0), dict(I=0), dict(E=0), dict(k=0), dict(t=2)):
+        assert _layer(**bad) == B.MOE_ERR_INVALID_ARG, bad
+    for bad in (dict(k=65), dict(E=1025), dict(T=2 ** 30, k=4), dict(H=2 ** 20, I=2 ** 11)):
+        assert _layer(nbytes=1 << 50, **bad) == B.MOE_ERR_UNSUPPORTED, bad
+    need = X.mx4_layer_scratch_size(4, 64, 32, 2)
+    assert need >= 4 * (32 + 4) + 8 * (64 + 16 + 4 + 128) and X.mx4_layer_scratch_size(4, 0, 32, 2) == 0
+    for bad in (dict(scratch=None), dict(nbytes=need - 1)):
+        assert _layer(**bad) == B.MOE_ERR_WORKSPACE, bad
+    for bad in (dict(h=P + 1), dict(w=P + 8), dict(off=P + 2), dict(rows_in=P + 2), dict(g=P + 2), dict(out=P + 2),
+                dict(scratch=P + 8), dict(ws=P + 128)):
+        assert _layer(**bad) == B.MOE_ERR_ALIGNMENT, bad
+    assert _layer(T=0, h=None, w=None, off=None, rows_in=None, g=None, out=None, scratch=None, nbytes=0) == B.MOE_OK
+
+
+def test_oracle_by_hand():
+    """The oracle against cases small enough to write down."""
+    import numpy as np
+
+    from oracle import experts as oe
+    ids, gates = np.array([[1, 0], [-1, 1], [0, 5]], np.int32), np.arange(1, 7, dtype=np.float32).reshape(3, 2)
+    off, tok, gw, rows = oe.sort_by_expert(ids, gates, 2)
+    assert off.tolist() == [0, 2, 4] and tok.tolist() == [0, 2, 0, 1, -1, -1]
+    assert gw.tolist() == [2, 5, 1, 4, 0, 0] and rows.tolist() == [[2, 0], [-1, 3], [1, -1]]
+    x = np.zeros((3, 33))
+    x[0, :5] = [6, 0.25, 0.75, -5, 2.5]      # 2^0: ties to the even code: 0, 1, -4, 2
+    x[0, 32] = 2.0 ** -130                   # the least scale, 2^-127: rounds to 0
+    x[1, :2] = [7, -1]                       # 2^0: 7 saturates to 6
+    x[2, 1] = np.inf
+    v = oe.mx4_values(*oe.mx4_quantize(x))
+    assert v.shape == (3, 64) and v[0, :5].tolist() == [6, 0, 1, -4, 2] and v[0, 32] == 0
+    assert v[1, :2].tolist() == [6, -1] and np.isnan(v[2, :32]).all() and (v[2, 32:] == 0).all()
