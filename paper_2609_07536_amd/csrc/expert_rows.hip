@@ -26,13 +26,15 @@ constexpr int kMaxExperts = 1024;
 // Up to kOneLaunch slots one workgroup does it all.  Beyond, a first launch
 // counts each chunk's experts and a second places the chunks, each workgroup
 // adding up all chunks' counts for itself (a few hundred KB at most, from the
-// L2): two launches without waits between workgroups.
+// L2): two launches without waits between workgroups.  Latency bounds both ways
+// (98304 slots move 2 MB, 0.4 us of a copy): 6 slots of 32 experts take 2.8 us of
+// GPU time, 98304 slots of 32 experts 3.0 + 6.8.
 constexpr int kOneLaunch = 4096;
 constexpr int kOneThreads = 1024;
 constexpr int kPlaceThreads = 256;
 // Slots of a chunk: as few as spread the work over many CUs, while what every
-// workgroup adds up (chunks times experts) stays small.  Measured (us, 512 / 1024 /
-// 2048 slots): 98304 slots of 32 experts 8.9 / 10.2 / 12.3, 262144 of 64 15.2 / 12.5 /
+// workgroup adds up (chunks times experts) stays small.  Measured (us a call, replayed
+// from a graph, 512 / 1024 / 2048 slots): 98304 slots of 32 experts 8.9 / 10.2 / 12.3, 262144 of 64 15.2 / 12.5 /
 // 13.0, 131072 of 256 20.8 / 15.9 / 15.2, 65536 of 1024 38 / 27 / 23.
 constexpr int kLeastChunk = 512, kChunk = 2048;   // (past kChunk: times what keeps them at most kMaxChunks)
 constexpr int kMaxChunks = 256;
@@ -276,7 +278,8 @@ __device__ __forceinline__ bool unit_at(long long unit, int T, int blocks, long 
   return *t < T;
 }
 
-// V: bytes of a chunk (16, or 1 for shorter rows); U chunks a lane
+// V: bytes of a chunk (16, or 1 for shorter rows); U chunks a lane.  Bound by memory;
+// a small call by latency: 777 tokens to their rows, 7.8 MB, 3.7 us.
 template <int V, int U>
 __global__ void __launch_bounds__(256) dispatch_kernel(const uint8_t* x, const int32_t* slot_rows,
                                                        uint8_t* out, int T, int topk, long long rows,
@@ -305,7 +308,10 @@ __global__ void __launch_bounds__(256) dispatch_kernel(const uint8_t* x, const i
   }
 }
 
-// Sums of a token's rows, weighted (combine) or not (the dispatch's gradient).
+// Sums of a token's rows, weighted (combine) or not (the dispatch's gradient), in fp32
+// in slot order, rounded once.  Bound by memory: every row is read once, in batches of
+// eight loads; the dispatch's gradient of 8192 tokens moves 168 MB in 32.9 us, 5.1 TB/s (a
+// copy reaches 4.9); 64 tokens combine in 3.4 us, latency.
 constexpr int kBatch = 8;   // rows whose loads are in flight together
 template <class In, class Out, bool kWeighted, int V>
 __global__ void __launch_bounds__(256) sum_rows_kernel(const In* y, const int32_t* slot_rows,
@@ -359,7 +365,9 @@ __device__ __forceinline__ float wave_sum(float v) {
 }
 
 // A wave takes a token: dout's columns stay in registers (64 V U of them at a
-// time) while its slots' rows of y come by and their gradients leave.
+// time) while its slots' rows of y come by and their gradients leave.  dgates' sum
+// is fp32, the lanes' parts joined in a fixed order; dy is rounded once.  Bound by
+// memory: y read and dy written once, 941 MB for 16384 tokens in 188 us, 5.0 TB/s.
 template <class DOut, class Y, int V, int U>
 __global__ void __launch_bounds__(256) combine_grad_kernel(const DOut* dout, const Y* y,
                                                            const int32_t* slot_rows, const float* gates,
