@@ -243,9 +243,11 @@ __global__ void __launch_bounds__(256) mx4_dequantize_kernel(const uint8_t* code
 //
 // What bounds large calls: 98304 rows (32 experts, K 2048, N 1408 with SwiGLU, 567
 // GFLOP) 210 us, 2.7 PFLOP/s, of which the loop over K is two thirds (16 stages of
-// 256 x 256 some 26 000 clocks, the matrix instructions alone 16 400), the rest the
-// stores of a finished tile and the wait for them: loads and stores are counted in
-// order, so the next tile's first stage waits for the stores before it.
+// 256 x 256 some 26 000 clocks, the matrix instructions alone 16 400), the rest a
+// finished tile's stores and the next one's start.  That the start waits for the
+// stores (loads and stores are counted in order) is not what costs: stores left under way
+// during the next tile's first two stages, with exact counts, gave the same outputs at
+// 196 -> 198 us here, 217 -> 213 for the down-projection (311 -> 307 with the combine).
 //
 // The stores are ordinary ones.  Non-temporal ones are faster alone (16384 tokens,
 // up 200 -> 189 us, down 226 -> 165) and slower with who reads them next (up and
