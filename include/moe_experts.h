@@ -147,9 +147,11 @@ int moe_mx4_product(const void* a_codes, const void* a_scales, const void* w_cod
  * contents do not matter, before or after. */
 size_t moe_mx4_layer_scratch_size(int32_t T, int32_t H, int32_t I, int32_t topk);
 
-/* The post-router layer with its experts in 4 bits, as five launches on stream:
- * hidden quantised; the up-projection with the token gather and SwiGLU; its
- * outputs (bf16) quantised; the down-projection (bf16); the combine.
+/* The post-router layer with its experts in 4 bits: hidden quantised; the
+ * up-projection with the token gather and SwiGLU; its outputs, rounded to bf16,
+ * quantised (by the up-projection itself in long calls, by a launch in short ones);
+ * the down-projection (bf16); the combine.  Four or five launches on stream, and the
+ * result is that of the separate calls bit for bit.
  *   hidden          device bf16 [T, H]
  *   w1              mx4 [E, 2 I, H]: an expert's I gate rows, then its I up rows
  *   w2              mx4 [E, H, I]

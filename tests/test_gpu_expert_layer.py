@@ -68,6 +68,32 @@ def test_layer_in_4_bits(gpu_lib, T, H, I, E, k, drop, dtype):
     assert torch.equal(again, out)
 
 
+@pytest.mark.parametrize("T,H,I,E,k,drop", [(2, 256, 96, 4, 2, 0.0), (700, 512, 704, 8, 2, 0.1), (1500, 1352, 336, 11, 3, 0.1),
+                                            (3000, 256, 72, 4, 2, 0.0), (6000, 128, 33, 3, 2, 0.3), (4000, 1024, 512, 8, 4, 0.0),
+                                            (20000, 64, 1, 2, 2, 0.0)])
+def test_layer_is_the_chain_of_its_calls(gpu_lib, T, H, I, E, k, drop):
+    """Bit for bit, whichever kernels each of them picks; one token holds a NaN, which
+    must reach its own output alone, and nothing beyond I columns."""
+    import torch
+
+    from paper_2609_07536_amd import experts as X
+    ids, gates, hidden, w1, w2 = _case(T, H, I, E, k, drop)
+    hidden[1, H // 2] = float("nan")
+    g, h, ids = torch.from_numpy(gates).cuda(), hidden.cuda(), torch.from_numpy(ids).cuda()
+    r = X.sort_by_expert(ids, g, E)
+    a, b = X.mx4_quantize_weights(w1.cuda()), X.mx4_quantize_weights(w2.cuda())
+    scratch = torch.full((X.mx4_layer_scratch_size(T, H, I, k),), 255, dtype=torch.uint8, device="cuda")
+    got = X.layer_forward_mx4(h, a, b, r, g, scratch=scratch)
+    x = torch.zeros(T * k, I, dtype=torch.bfloat16, device="cuda")
+    X.mx4_product(X.mx4_quantize(h), a, r.expert_offsets, T * k, row_ids=r.token_ids, swiglu=True, out=x)
+    y = torch.zeros(T * k, H, dtype=torch.bfloat16, device="cuda")
+    X.mx4_product(X.mx4_quantize(x), b, r.expert_offsets, T * k, out=y)
+    want = X.combine_rows(y, r.slot_rows, g)
+    assert torch.equal(got.view(torch.int32), want.view(torch.int32))
+    nan = torch.isnan(got).any(1)
+    assert bool(nan[1]) == bool((r.slot_rows[1] >= 0).any()) and int(nan.sum()) <= 1
+
+
 def test_layer_refusals(gpu_lib):
     import torch
 
