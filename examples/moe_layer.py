@@ -1,6 +1,6 @@
 """A mixture-of-experts layer from its router on, served and trained.
 
-    python examples/moe_layer.py [--tokens 512] [--steps 20]
+    python examples/moe_layer.py [--tokens 1024] [--steps 20]
 
 Serving: the router's top-k is sorted by expert, and the layer runs with its
 experts in bf16 (binding.layer_forward) and in 4 bits (experts.layer_forward_mx4);
@@ -106,7 +106,7 @@ def train(T, steps, H=256, I=128, E=8, topk=2):
 
 if __name__ == "__main__":
     ap = argparse.ArgumentParser()
-    ap.add_argument("--tokens", type=int, default=512)
+    ap.add_argument("--tokens", type=int, default=1024)
     ap.add_argument("--steps", type=int, default=20)
     a = ap.parse_args()
     serve(a.tokens)

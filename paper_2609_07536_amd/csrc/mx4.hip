@@ -377,7 +377,7 @@ __device__ __forceinline__ int all_tiles(const MxArgs& a) {
 // kCodes (with SwiGLU): the output, rounded to bf16 as it would be stored, leaves in 4
 // bits, as mx4_quantize_kernel makes them: four lanes hold a block's 32 columns.  The
 // layer, replayed from a graph, against a launch that reads the bf16 and quantises it
-// (32 experts of 2048 x 704, top 6): 512 tokens 40.3 -> 38.1 us, 4096 156.8 -> 144.3, 16384
+// (32 experts of 2048 x 704, top 6): 1024 tokens 56.5 -> 53.5 us, 4096 156.8 -> 144.3, 16384
 // 547.9 -> 539.7; over four shapes 1.5 to 8% less.  Thin kernels hold 16 columns a wave,
 // half a block, and leave it to that launch.
 template <class C, bool kSwiglu, bool kCodes>

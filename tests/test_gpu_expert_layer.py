@@ -94,6 +94,42 @@ def test_layer_is_the_chain_of_its_calls(gpu_lib, T, H, I, E, k, drop):
     assert bool(nan[1]) == bool((r.slot_rows[1] >= 0).any()) and int(nan.sum()) <= 1
 
 
+def test_serving_on_a_stream_and_in_a_graph(gpu_lib):
+    """Sort and layer on a stream of their own, and replayed from a graph whose inputs
+    change between replays, against the same calls made eagerly."""
+    import torch
+
+    from paper_2609_07536_amd import experts as X
+    T, H, I, E, k = 600, 256, 96, 4, 2
+    w1, w2 = _case(T, H, I, E, k, 0.0)[3:]
+    a, b = X.mx4_quantize_weights(w1.cuda()), X.mx4_quantize_weights(w2.cuda())
+    inputs = []
+    for seed in range(3):
+        ids, gates, hidden = _case(T, H, I, E, k, 0.1, seed)[:3]
+        inputs.append((torch.from_numpy(ids).cuda(), torch.from_numpy(gates).cuda(), hidden.cuda()))
+
+    def serve(ids, g, h, stream=None):
+        return X.layer_forward_mx4(h, a, b, X.sort_by_expert(ids, g, E, stream=stream), g, stream=stream)
+    eager = [serve(*v).clone() for v in inputs]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        assert all(torch.equal(serve(*v), want) for v, want in zip(inputs, eager))
+    side.synchronize()
+    held = tuple(t.clone() for t in inputs[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = serve(*held)
+    for turn in range(5):
+        for t, new in zip(held, inputs[turn % 3]):
+            t.copy_(new)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager[turn % 3]), turn
+        serve(*inputs[(turn + 1) % 3])   # (the program's own work between the replays)
+
+
 def test_layer_refusals(gpu_lib):
     import torch
 
