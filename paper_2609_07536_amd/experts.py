@@ -3,7 +3,9 @@
 
 Tensors are contiguous and on the GPU.  Every function takes ``stream`` (a
 torch stream; default: the current one) and only enqueues work on it; outputs
-that are not given with ``out`` are allocated for that stream.  ``workspace``
+that are not given with ``out`` are allocated for that stream, and ones that are
+count as changed in place (autograd refuses a backward pass that had saved what
+was there before).  ``workspace``
 (a ``binding.Workspace`` of at least 512 bytes) is where the row operators
 record bad entries of ``slot_rows`` or ``row_ids`` for ``Workspace.status``.
 """
@@ -91,6 +93,10 @@ def _empty(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+# The library writes through raw pointers, which torch does not see.
+_written = torch.autograd.graph.increment_version
+
+
 def _done(r, what):
     if r < 0:
         raise MoeError(r, what)
@@ -118,7 +124,7 @@ def sort_by_expert(expert_ids, gates, E: int, first_expert: int = 0, out: Option
     are slots without a row.  scratch: uint8, at least sort_scratch_size bytes."""
     T, topk = shape = _two(expert_ids, "expert_ids", _I32)
     _check(gates, "gates", shape, _F32)
-    n = T * topk
+    n, given = T * topk, out
     if out is None:
         dev = expert_ids.device
         out = Routing(_empty((E + 1,), torch.int32, dev, stream), _empty((n,), torch.int32, dev, stream),
@@ -140,6 +146,8 @@ def sort_by_expert(expert_ids, gates, E: int, first_expert: int = 0, out: Option
                              scratch.data_ptr() if room else None, room, _stream(stream))
     if r < 0:
         raise MoeError(r, "moe_sort_by_expert")
+    if given is not None:
+        _written(given)
     return out
 
 
@@ -155,6 +163,7 @@ def dispatch_rows(x, slot_rows, rows: int, out=None, workspace: Optional[Workspa
     H = _two(x, "x", dtypes)[1]
     if x.shape[0] != T:
         raise TypeError(f"x: {x.shape[0]} rows, slot_rows {T}")
+    given = out
     if out is None:
         out = _empty((rows, H), x.dtype, x.device, stream)
     else:
@@ -163,6 +172,8 @@ def dispatch_rows(x, slot_rows, rows: int, out=None, workspace: Optional[Workspa
                                 H * x.element_size(), _status_word(workspace), _stream(stream))
     if r < 0:
         raise MoeError(r, "moe_dispatch_rows")
+    if given is not None:
+        _written(given)
     return out
 
 
@@ -171,6 +182,7 @@ def dispatch_rows_grad(d, slot_rows, out=None, workspace: Optional[Workspace] = 
     or `out`'s): the sum of each token's rows, in fp32, rounded once."""
     T, topk = _two(slot_rows, "slot_rows", _I32)
     rows, H = _two(d, "d", _FLOAT)
+    given = out
     if out is None:
         out = _empty((T, H), d.dtype, d.device, stream)
     else:
@@ -179,6 +191,8 @@ def dispatch_rows_grad(d, slot_rows, out=None, workspace: Optional[Workspace] = 
                                      _TYPES[d.dtype], _TYPES[out.dtype], _status_word(workspace), _stream(stream))
     if r < 0:
         raise MoeError(r, "moe_dispatch_rows_grad")
+    if given is not None:
+        _written(given)
     return out
 
 
@@ -190,6 +204,7 @@ def combine_rows(y, slot_rows, gates, out=None, dtype=torch.float32, workspace: 
     T, topk = shape = _two(slot_rows, "slot_rows", _I32)
     _check(gates, "gates", shape, _F32)
     rows, H = _two(y, "y", _FLOAT)
+    given = out
     if out is None:
         out = _empty((T, H), dtype, y.device, stream)
     _check(out, "out", (T, H), _FLOAT)
@@ -197,6 +212,8 @@ def combine_rows(y, slot_rows, gates, out=None, dtype=torch.float32, workspace: 
                                H, _TYPES[y.dtype], _TYPES[out.dtype], _status_word(workspace), _stream(stream))
     if r < 0:
         raise MoeError(r, "moe_combine_rows")
+    if given is not None:
+        _written(given)
     return out
 
 
@@ -219,6 +236,8 @@ def combine_rows_grad(d_out, y, slot_rows, gates, out=None, workspace: Optional[
                                     _TYPES[y.dtype], _status_word(workspace), _stream(stream))
     if r < 0:
         raise MoeError(r, "moe_combine_rows_grad")
+    if out is not None:
+        _written((dy, dgates))
     return dy, dgates
 
 
@@ -262,11 +281,14 @@ def mx4_quantize(x, out: Optional[MX4] = None, stream=None) -> MX4:
     if len(shape) < 1:
         raise TypeError("x: expected at least one dimension")
     K, lead = shape[-1], shape[:-1]
+    given = out
     out = _mx4_out(out, lead, K, x.device, stream)
     r = lib().moe_mx4_quantize(x.data_ptr(), out[0].data_ptr(), out[1].data_ptr(), lead.numel(), K,
                                _TYPES[x.dtype], _stream(stream))
     if r < 0:
         raise MoeError(r, "moe_mx4_quantize")
+    if given is not None:
+        _written(given[:2])
     return out
 
 
@@ -277,9 +299,12 @@ def mx4_quantize_weights(w, out: Optional[MX4] = None, stream=None) -> MX4:
     if w.dim() != 3:
         raise TypeError(f"w: expected [E, K, N], got {tuple(w.shape)}")
     E, K, N = w.shape
+    given = out
     out = _mx4_out(out, (E, N), K, w.device, stream)
     _done(lib().moe_mx4_quantize_weights(w.data_ptr(), out[0].data_ptr(), out[1].data_ptr(), E, K, N,
                                          _TYPES[w.dtype], _stream(stream)), "moe_mx4_quantize_weights")
+    if given is not None:
+        _written(given[:2])
     return out
 
 
@@ -288,6 +313,7 @@ def mx4_dequantize(m: MX4, out=None, dtype=torch.bfloat16, stream=None):
     codes, scales, K = m
     lead = codes.shape[:-1]
     _mx4_check(m, "m", lead)
+    given = out
     if out is None:
         out = _empty((*lead, K), dtype, codes.device, stream)
     _check(out, "out", (*lead, K), _FLOAT)
@@ -295,6 +321,8 @@ def mx4_dequantize(m: MX4, out=None, dtype=torch.bfloat16, stream=None):
                                  _TYPES[out.dtype], _stream(stream))
     if r < 0:
         raise MoeError(r, "moe_mx4_dequantize")
+    if given is not None:
+        _written(given)
     return out
 
 
@@ -319,6 +347,7 @@ def mx4_product(a: MX4, w: MX4, expert_offsets, rows: int, row_ids=None, swiglu:
     if rows > have:
         raise TypeError(f"{rows} rows, but {have} " + ("of a" if row_ids is None else "row_ids"))
     shape = (rows, N // 2 if swiglu else N)
+    given = out
     if out is None:
         out = _empty(shape, torch.bfloat16, a_codes.device, stream)
     else:
@@ -329,6 +358,8 @@ def mx4_product(a: MX4, w: MX4, expert_offsets, rows: int, row_ids=None, swiglu:
                               _stream(stream))
     if r < 0:
         raise MoeError(r, "moe_mx4_product")
+    if given is not None:
+        _written(given)
     return out
 
 
@@ -359,6 +390,7 @@ def layer_forward_mx4(hidden, w1: MX4, w2: MX4, routing: Routing, gates, out=Non
     _check(gates, "gates", shape, _F32)
     _check(offsets, "expert_offsets", (E + 1,), _I32)
     _check(token_ids, "token_ids", (T * topk,), _I32)
+    given = out
     if out is None:
         out = _empty((T, H), dtype, hidden.device, stream)
     _check(out, "out", (T, H), _FLOAT)
@@ -372,4 +404,6 @@ def layer_forward_mx4(hidden, w1: MX4, w2: MX4, routing: Routing, gates, out=Non
                                 scratch.data_ptr(), scratch.numel(), _status_word(workspace), _stream(stream))
     if r < 0:
         raise MoeError(r, "moe_mx4_layer_forward")
+    if given is not None:
+        _written(given)
     return out
