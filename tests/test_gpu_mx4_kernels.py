@@ -1,0 +1,191 @@
+"""GPU: every kernel that a 4-bit product can run as, against the 64-bit oracle (the
+shapes: mx4_shapes.py, which test_mx4_launches.py holds against the library's rule).
+
+Operands are random codes and scale bytes.  Tolerances: as in test_gpu_mx4.py, an
+fp32 sum of K exact terms is off by at most K 2^-24 times the sum of their
+magnitudes, rounding to bf16 by 2^-8 of the value; with SwiGLU (1.1 |u| + |silu(g)| +
+d) d for an error d of both inputs, and another 2^-8 for the activation.
+"""
+import numpy as np
+import pytest
+
+import mx4_shapes
+from oracle import experts as oe
+
+pytestmark = pytest.mark.gpu
+NAMES = ["thin16k8", "thin16k16", "thin32", "thin64", "tile128", "tile256"]
+
+
+def _random(shape, K, exponent, gen):
+    """Random codes and scale bytes of [*shape, K] around 2^exponent; what no element or
+    block has is as the layout says (codes of zeros) and, for pad bytes, 255."""
+    import torch
+
+    from paper_2609_07536_amd import experts as X
+    code_shape, scale_shape = X._mx4_shapes(shape, K)
+    codes = torch.randint(0, 256, code_shape, dtype=torch.uint8, device="cuda", generator=gen)
+    scales = torch.randint(124 + exponent, 131 + exponent, scale_shape, dtype=torch.uint8, device="cuda", generator=gen)
+    codes[..., (K + 1) // 2:] = 0
+    if K % 2:
+        codes[..., K // 2] &= 15
+    scales[..., -(-K // 32):] = 255
+    return X.MX4(codes, scales, K)
+
+
+def _values(m):
+    """The oracle's values of `m`, as float64 on the GPU."""
+    import torch
+    c, s = oe.mx4_unpack(m.codes.cpu().numpy(), m.scales.cpu().numpy())
+    return torch.from_numpy(oe.mx4_values(c, s)[..., :m.K]).cuda()
+
+
+def _wanted(a, w, counts, ids, swiglu):
+    """(product or activation, bound of its error) [rows in use, ...] in 64 bits."""
+    import torch
+    M, E = sum(counts), len(counts)
+    x = _values(a._replace(codes=a.codes[:M], scales=a.scales[:M])) if ids is None else _values(a)[ids[:M].long()]
+    y, S = [], []
+    for e, rows in enumerate(x.split(list(counts))):
+        if len(rows):
+            v = _values(w._replace(codes=w.codes[e], scales=w.scales[e])).T.contiguous()
+            y.append(rows @ v)
+            S.append(rows.abs() @ v.abs())
+    N = w.codes.shape[1]
+    y, d = torch.cat(y), w.K * 2.0 ** -24 * torch.cat(S)
+    if not swiglu:
+        return y, d + 2.0 ** -8 * y.abs()
+    g, u = y[:, :N // 2], y[:, N // 2:]
+    silu, d = g / (1 + torch.exp(-g)), torch.maximum(d[:, :N // 2], d[:, N // 2:])
+    assert E == w.codes.shape[0]
+    return silu * u, (1.1 * u.abs() + silu.abs() + d) * d + 2 * 2.0 ** -8 * (silu * u).abs()
+
+
+def _check(kernel, counts, K, N, rows, swiglu, gather=0, seed=0, a=None, w=None, ids=None):
+    import torch
+
+    from paper_2609_07536_amd import binding as B
+    from paper_2609_07536_amd import experts as X
+    gen = torch.Generator(device="cuda").manual_seed(1000 * seed + K + N + rows)
+    M, E = sum(counts), len(counts)
+    assert M <= rows
+    a = _random((gather or rows,), K, 0, gen) if a is None else a
+    w = _random((E, N), K, -int(np.log2(K) / 2) - 2, gen) if w is None else w
+    if gather and ids is None:
+        ids = torch.randint(0, gather, (rows,), dtype=torch.int32, device="cuda", generator=gen)
+    off = torch.tensor([0, *np.cumsum(counts).tolist()], dtype=torch.int32, device="cuda")
+    out = torch.full((rows, N // 2 if swiglu else N), 7.0, dtype=torch.bfloat16, device="cuda")
+    ws = B.Workspace(512)
+    X.mx4_product(a, w, off, rows, row_ids=ids, swiglu=swiglu, out=out, workspace=ws)
+    assert ws.status() == 0
+    want, tol = _wanted(a, w, counts, ids, swiglu)
+    err = (out[:M].double() - want).abs()
+    what = (NAMES[kernel], counts[:8], K, N, rows, swiglu, gather)
+    assert bool((err <= tol).all()), (what, float((err / tol).max()), torch.nonzero(~(err <= tol))[:5].tolist())
+    assert bool((out[M:] == 7).all()), what
+    return out
+
+
+def _ways(N):
+    """Plain and gathered, without SwiGLU and (even N) with it."""
+    return [(False, 0), (False, 60)] + ([(True, 0), (True, 60)] if N % 2 == 0 else [])
+
+
+def _of(what, kernel):
+    return [s[1:] for s in mx4_shapes.shapes(what) if s[0] == kernel]
+
+
+@pytest.mark.parametrize("kernel", range(6), ids=NAMES)
+def test_over_reductions(gpu_lib, kernel):
+    for E, K, N, rows in _of(mx4_shapes.REDUCTIONS, kernel):
+        for i, (swiglu, gather) in enumerate(_ways(N)):
+            _check(kernel, [[300, 0, 129, 1], [0, 17, 0, 258]][i % 2], K, N, rows, swiglu, gather, seed=i)
+
+
+@pytest.mark.parametrize("kernel", range(6), ids=NAMES)
+def test_over_columns(gpu_lib, kernel):
+    for E, K, N, rows in _of(mx4_shapes.COLUMNS, kernel):
+        for i, (swiglu, gather) in enumerate(_ways(N)):
+            _check(kernel, [[2, 130, 0, 1], [260, 0, 33, 16]][i % 2], K, N, rows, swiglu, gather, seed=i)
+
+
+COUNTS = {1: [[1], [700], [1500]], 3: [[63, 64, 65]], 4: [[0, 0, 1, 0], [255, 0, 256, 257], [511, 513, 3, 0]],
+          5: [[0, 127, 128, 129, 1]], 8: [[2, 0, 15, 16, 17, 31, 32, 33]], 32: [[1] * 32], 100: [[5] * 100],
+          600: [[int(i % 10 == 3) for i in range(600)]], 1024: [[i * 7 % 5 % 4 for i in range(1024)], [0] * 1023 + [300]]}
+
+
+@pytest.mark.parametrize("kernel", range(6), ids=NAMES)
+def test_over_experts(gpu_lib, kernel):
+    for E, K, N, rows in _of(mx4_shapes.EXPERTS, kernel):
+        for counts in COUNTS[E]:
+            assert len(counts) == E
+            for i, (swiglu, gather) in enumerate(_ways(N)):
+                if E <= 100 or i in (0, 3):
+                    _check(kernel, counts, K, N, rows, swiglu, gather, seed=i)
+
+
+@pytest.mark.parametrize("kernel,counts,K,N,rows", mx4_shapes.SEVERAL, ids=str)
+@pytest.mark.parametrize("swiglu", [False, True])
+def test_several_tiles_per_workgroup(gpu_lib, kernel, counts, K, N, rows, swiglu):
+    """Each workgroup takes its next tile while it stores the last one."""
+    _check(kernel, counts, K, N, rows, swiglu, gather=500 if swiglu else 0)
+
+
+@pytest.mark.parametrize("kernel", range(6), ids=NAMES)
+def test_nan_blocks_reach_their_rows_and_columns(gpu_lib, kernel):
+    """... and nothing else: other rows, columns and experts are bit for bit the same."""
+    import torch
+
+    from paper_2609_07536_amd import experts as X
+    _, E, K, N, rows = max((s for s in mx4_shapes.shapes(mx4_shapes.REDUCTIONS) if s[0] == kernel and s[2] <= 2080),
+                           key=lambda s: s[2])
+    counts, gen = [200, 0, 70, 1], torch.Generator(device="cuda").manual_seed(5)
+    a, w = _random((rows,), K, 0, gen), _random((E, N), K, -7, gen)
+    off = torch.tensor([0, *np.cumsum(counts).tolist()], dtype=torch.int32, device="cuda")
+    last = -(-K // 32) - 1
+    for swiglu in (False, True):
+        before = X.mx4_product(a, w, off, rows, swiglu=swiglu)[:271]
+        na, nw = (X.MX4(t.codes.clone(), t.scales.clone(), K) for t in (a, w))
+        na.scales[3, 0] = na.scales[150, last] = na.scales[270, last // 2] = 255
+        nw.scales[0, 5, last] = nw.scales[2, N - 1, 0] = nw.scales[1, 9, 0] = 255
+        got = X.mx4_product(na, nw, off, rows, swiglu=swiglu)[:271]
+        bad = torch.zeros_like(got, dtype=torch.bool)
+        bad[3] = bad[150] = bad[270] = True
+        bad[:200, 5] = True
+        bad[200:270, (N // 2 if swiglu else N) - 1] = True
+        assert torch.equal(torch.isnan(got), bad)
+        assert torch.equal(got[~bad], before[~bad])
+
+
+@pytest.mark.parametrize("kernel", range(6), ids=NAMES)
+def test_bad_row_ids_and_offsets(gpu_lib, kernel):
+    """Bad ids are zeros and flagged, wherever they are in a tile; offsets that are no
+    prefix of [0, rows] are clamped and flagged."""
+    import torch
+
+    from paper_2609_07536_amd import binding as B
+    from paper_2609_07536_amd import experts as X
+    E, K, N, rows = _of(mx4_shapes.REDUCTIONS, kernel)[-1]
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    a, w = _random((50,), K, 0, gen), _random((E, N), K, -5, gen)
+    ids = torch.randint(0, 50, (rows,), dtype=torch.int32, device="cuda", generator=gen)
+    off = torch.tensor([0, 150, 150, 290, 300], dtype=torch.int32, device="cuda")
+    ws = B.Workspace(512)
+    want = X.mx4_product(a, w, off, rows, row_ids=ids, workspace=ws)[:300]
+    assert ws.status() == 0
+    where = [0, 1, 77, 149, 150, 289, 290, 299]
+    wrong = ids.clone()
+    wrong[where] = torch.tensor([-1, 50, -2 ** 31, 2 ** 31 - 1] * 2, dtype=torch.int32, device="cuda")
+    for space in (None, ws):
+        got = X.mx4_product(a, w, off, rows, row_ids=wrong, workspace=space)[:300]
+        good = torch.ones(300, dtype=torch.bool, device="cuda")
+        good[where] = False
+        assert torch.equal(got[good], want[good]) and bool((got[~good] == 0).all())
+    assert ws.status(clear=True) == B.MOE_ERR_BAD_ROUTING
+    # ids past the rows in use are nobody's
+    ids[300:] = -5
+    assert torch.equal(X.mx4_product(a, w, off, rows, row_ids=ids, workspace=ws)[:300], want)
+    assert ws.status() == 0
+    for bad in ([0, 150, 150, 290, rows + 1], [1, 150, 150, 290, 300], [0, 150, 140, 290, 300]):
+        X.mx4_product(a, w, torch.tensor(bad, dtype=torch.int32, device="cuda"), rows, row_ids=ids.clamp(min=0),
+                      workspace=ws)
+        assert ws.status(clear=True) == B.MOE_ERR_BAD_ROUTING, bad
