@@ -405,12 +405,13 @@ __global__ void __launch_bounds__(C::kThr, C::R * C::NW / 4) mx4_product_kernel(
   const uint32_t pitch = (uint32_t)a.KB * kBlockBytes;
   const int KT = (a.KB + 3) / 4;
   const i32x4 ra = buffer_rsrc(a.a, (long long)a.a_rows * pitch), ras = buffer_rsrc(a.as, (long long)a.a_rows * a.KS);
-  const i32x4 rids = buffer_rsrc(a.row_ids, a.row_ids ? a.rows * 4 : 0);
   i32x4 rw, rws;
 
-  auto issue_ids = [&](const Tile& t) MX_INLINE {   // a tile's row ids, four a lane
+  // a tile's row ids, four a lane (by a resource of the tile's own: an offset from the
+  // first row's would pass 32 bits)
+  auto issue_ids = [&](const Tile& t) MX_INLINE {
     if (a.row_ids && wave == 0 && 4 * lane < C::BM)
-      dma16(rids, 4 * lane < t.rows_valid ? 4u * (uint32_t)(t.r0 + 4 * lane) : kOutOfRange, lds + C::kIds);
+      dma16(buffer_rsrc(a.row_ids + t.r0, 4ll * t.rows_valid), 16u * (uint32_t)lane, lds + C::kIds);
   };
   // tile row i (BM rows of a, then BN of w) to its row in memory, or -1
   auto row_of = [&](const Tile& t, int i) MX_INLINE -> int {
