@@ -93,6 +93,14 @@ def _empty(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+# The library's sizes are 32 bits, and ctypes cuts a larger int without a word.
+_MOST = 2 ** 31 - 1
+
+
+def _too_large(what):
+    raise MoeError(_b.MOE_ERR_UNSUPPORTED, what)
+
+
 # The library writes through raw pointers, which torch does not see.
 _written = torch.autograd.graph.increment_version
 
@@ -124,6 +132,8 @@ def sort_by_expert(expert_ids, gates, E: int, first_expert: int = 0, out: Option
     are slots without a row.  scratch: uint8, at least sort_scratch_size bytes."""
     T, topk = shape = _two(expert_ids, "expert_ids", _I32)
     _check(gates, "gates", shape, _F32)
+    if (T | topk | E) > _MOST or not -_MOST <= first_expert + 1 <= _MOST + 1:
+        _too_large("moe_sort_by_expert")
     n, given = T * topk, out
     if out is None:
         dev = expert_ids.device
@@ -152,7 +162,7 @@ def sort_by_expert(expert_ids, gates, E: int, first_expert: int = 0, out: Option
 
 
 def sort_scratch_size(T: int, topk: int, E: int) -> int:
-    return int(lib().moe_sort_scratch_size(T, topk, E))
+    return 0 if max(T, topk, E) > _MOST else int(lib().moe_sort_scratch_size(T, topk, E))
 
 
 def dispatch_rows(x, slot_rows, rows: int, out=None, workspace: Optional[Workspace] = None, stream=None):
@@ -163,6 +173,8 @@ def dispatch_rows(x, slot_rows, rows: int, out=None, workspace: Optional[Workspa
     H = _two(x, "x", dtypes)[1]
     if x.shape[0] != T:
         raise TypeError(f"x: {x.shape[0]} rows, slot_rows {T}")
+    if (T | topk) > _MOST:
+        _too_large("moe_dispatch_rows")
     given = out
     if out is None:
         out = _empty((rows, H), x.dtype, x.device, stream)
@@ -182,6 +194,8 @@ def dispatch_rows_grad(d, slot_rows, out=None, workspace: Optional[Workspace] = 
     or `out`'s): the sum of each token's rows, in fp32, rounded once."""
     T, topk = _two(slot_rows, "slot_rows", _I32)
     rows, H = _two(d, "d", _FLOAT)
+    if (T | topk | H) > _MOST:
+        _too_large("moe_dispatch_rows_grad")
     given = out
     if out is None:
         out = _empty((T, H), d.dtype, d.device, stream)
@@ -204,6 +218,8 @@ def combine_rows(y, slot_rows, gates, out=None, dtype=torch.float32, workspace: 
     T, topk = shape = _two(slot_rows, "slot_rows", _I32)
     _check(gates, "gates", shape, _F32)
     rows, H = _two(y, "y", _FLOAT)
+    if (T | topk | H) > _MOST:
+        _too_large("moe_combine_rows")
     given = out
     if out is None:
         out = _empty((T, H), dtype, y.device, stream)
@@ -223,6 +239,8 @@ def combine_rows_grad(d_out, y, slot_rows, gates, out=None, workspace: Optional[
     T, topk = shape = _two(slot_rows, "slot_rows", _I32)
     _check(gates, "gates", shape, _F32)
     rows, H = _two(y, "y", _FLOAT)
+    if (T | topk | H) > _MOST:
+        _too_large("moe_combine_rows_grad")
     _check(d_out, "d_out", (T, H), _FLOAT)
     if out is None:
         dy = _empty((rows, H), y.dtype, y.device, stream)
@@ -281,6 +299,8 @@ def mx4_quantize(x, out: Optional[MX4] = None, stream=None) -> MX4:
     if len(shape) < 1:
         raise TypeError("x: expected at least one dimension")
     K, lead = shape[-1], shape[:-1]
+    if K > _MOST:
+        _too_large("moe_mx4_quantize")
     given = out
     out = _mx4_out(out, lead, K, x.device, stream)
     r = lib().moe_mx4_quantize(x.data_ptr(), out[0].data_ptr(), out[1].data_ptr(), lead.numel(), K,
@@ -299,6 +319,8 @@ def mx4_quantize_weights(w, out: Optional[MX4] = None, stream=None) -> MX4:
     if w.dim() != 3:
         raise TypeError(f"w: expected [E, K, N], got {tuple(w.shape)}")
     E, K, N = w.shape
+    if (E | K | N) > _MOST:
+        _too_large("moe_mx4_quantize_weights")
     given = out
     out = _mx4_out(out, (E, N), K, w.device, stream)
     _done(lib().moe_mx4_quantize_weights(w.data_ptr(), out[0].data_ptr(), out[1].data_ptr(), E, K, N,
@@ -313,6 +335,8 @@ def mx4_dequantize(m: MX4, out=None, dtype=torch.bfloat16, stream=None):
     codes, scales, K = m
     lead = codes.shape[:-1]
     _mx4_check(m, "m", lead)
+    if K > _MOST:
+        _too_large("moe_mx4_dequantize")
     given = out
     if out is None:
         out = _empty((*lead, K), dtype, codes.device, stream)
@@ -338,6 +362,8 @@ def mx4_product(a: MX4, w: MX4, expert_offsets, rows: int, row_ids=None, swiglu:
         raise TypeError(f"expected a [rows, K] and w [E, N, K], got {tuple(a_shape)}, K = {K}, and "
                         f"{tuple(w_shape)}, K = {w.K}")
     a_rows, E, N = a_shape[0], w_shape[0], w_shape[1]
+    if (K | E | N) > _MOST:
+        _too_large("moe_mx4_product")
     _mx4_check(a, "a", (a_rows,))
     _mx4_check(w, "w", (E, N))
     _check(expert_offsets, "expert_offsets", (E + 1,), _I32)
@@ -364,7 +390,7 @@ def mx4_product(a: MX4, w: MX4, expert_offsets, rows: int, row_ids=None, swiglu:
 
 
 def mx4_layer_scratch_size(T: int, H: int, I: int, topk: int) -> int:
-    return int(lib().moe_mx4_layer_scratch_size(T, H, I, topk))
+    return 0 if max(T, H, I, topk) > _MOST else int(lib().moe_mx4_layer_scratch_size(T, H, I, topk))
 
 
 def layer_forward_mx4(hidden, w1: MX4, w2: MX4, routing: Routing, gates, out=None, dtype=torch.float32,
@@ -387,6 +413,8 @@ def layer_forward_mx4(hidden, w1: MX4, w2: MX4, routing: Routing, gates, out=Non
     topk = shape[1]
     if shape[0] != T:
         raise TypeError(f"slot_rows: {shape[0]} tokens, hidden {T}")
+    if (T | H | I | E | topk) > _MOST:
+        _too_large("moe_mx4_layer_forward")
     _check(gates, "gates", shape, _F32)
     _check(offsets, "expert_offsets", (E + 1,), _I32)
     _check(token_ids, "token_ids", (T * topk,), _I32)
