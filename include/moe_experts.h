@@ -27,6 +27,9 @@
  * 512 bytes, of which only the status word is used) is not NULL,
  * moe_gemm2_status reports MOE_ERR_BAD_ROUTING.  Rows that no slot has are
  * not written; a row that several slots have is written by one of them.
+ * T, rows >= 0, 1 <= topk <= 64, 1 <= H < 2^31 - 4096 (elements; dispatch: bytes
+ * of a row below 2^31), rows < 2^31, else MOE_ERR_INVALID_ARG or, past an upper
+ * limit, MOE_ERR_UNSUPPORTED.
  * Sums over slots are taken in fp32 in slot order and rounded once (round to
  * nearest even) to the output's type, so results do not vary from run to
  * run.
@@ -81,8 +84,7 @@ int moe_sort_by_expert(const int32_t* expert_ids, const float* gates, int32_t* e
 
 /* ---- rows to the experts and back --------------------------------------- */
 
-/* x [T, row_bytes] to out [rows, row_bytes]; the type does not matter.
- * T, rows >= 0, row_bytes >= 1, 1 <= topk <= 64. */
+/* x [T, row_bytes] to out [rows, row_bytes]; the type does not matter. */
 int moe_dispatch_rows(const void* x, const int32_t* slot_rows, void* out, int32_t T, int32_t topk,
                       int64_t rows, int64_t row_bytes, void* workspace, void* stream);
 

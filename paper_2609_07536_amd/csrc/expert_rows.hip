@@ -434,6 +434,9 @@ unsigned blocks_for(long long units) {
   return (unsigned)(n < kMaxBlocks ? n : kMaxBlocks);
 }
 
+// Columns that the kernels count in 32 bits, with what lies past the last step of theirs.
+constexpr int64_t kMaxColumns = INT32_MAX - 4096;
+
 // What the row operators have in common.
 int check_rows(const int32_t* slot_rows, int32_t T, int32_t topk, int64_t rows, int64_t width,
                const void* workspace) {
@@ -484,6 +487,7 @@ int sum_rows(bool weighted, const void* y, const int32_t* slot_rows, const float
              void* stream) {
   const int bad = check_rows(slot_rows, T, topk, rows, H, workspace);
   if (bad) return bad;
+  if (H > kMaxColumns) return MOE_ERR_UNSUPPORTED;
   if (!type_ok(y_type) || !type_ok(out_type)) return MOE_ERR_INVALID_ARG;
   if (T == 0) return MOE_OK;
   if (!out || (rows > 0 && !y) || (weighted && !gates)) return MOE_ERR_INVALID_ARG;
@@ -596,6 +600,7 @@ extern "C" int moe_combine_rows_grad(const void* dout, const void* y, const int3
                                      int32_t dout_type, int32_t y_type, void* workspace, void* stream) {
   const int bad = check_rows(slot_rows, T, topk, rows, H, workspace);
   if (bad) return bad;
+  if (H > kMaxColumns) return MOE_ERR_UNSUPPORTED;
   if (!type_ok(dout_type) || !type_ok(y_type)) return MOE_ERR_INVALID_ARG;
   if (T == 0) return MOE_OK;
   if (!dout || !gates || !dgates || (rows > 0 && (!y || !dy))) return MOE_ERR_INVALID_ARG;

@@ -100,3 +100,16 @@ def test_sizes_of_scratch_past_32_bits():
     assert X.sort_scratch_size(16384, BIG + 6, 32) == 0
     for big in ((BIG + 4, 64, 32, 2), (4, BIG + 64, 32, 2), (4, 64, BIG + 32, 2), (4, 64, 32, BIG + 2)):
         assert X.mx4_layer_scratch_size(*big) == 0
+
+
+P = 1 << 20   # an aligned address that no refused call touches
+
+
+def test_columns_near_2_to_31():
+    """Past what the kernels' 32-bit steps over the columns hold (a loop over 2048 of
+    them at a time passes 2^31 - 1 before it ends)."""
+    L = X.lib()
+    for H, code in ((2 ** 31 - 1, B.MOE_ERR_UNSUPPORTED), (2 ** 31 - 4096, B.MOE_ERR_UNSUPPORTED), (0, B.MOE_ERR_INVALID_ARG)):
+        assert L.moe_dispatch_rows_grad(P, P, P, 1, 1, 1, H, 0, 0, None, None) == code
+        assert L.moe_combine_rows(P, P, P, P, 1, 1, 1, H, 0, 0, None, None) == code
+        assert L.moe_combine_rows_grad(P, P, P, P, P, P, 1, 1, 1, H, 0, 0, None, None) == code
