@@ -110,18 +110,21 @@ int moe_combine_rows_grad(const void* dout, const void* y, const int32_t* slot_r
 /* ---- microscaled 4-bit floating point ----------------------------------------- */
 
 /* x [rows, K] of x_type (aligned to its elements) to codes and scales (format
- * above), every byte of which is written.  rows >= 0, K >= 1. */
+ * above), every byte of which is written.  rows >= 0, 1 <= K < 2^31 - 256, and rows
+ * times K (rounded up to 32) below 2^35, else MOE_ERR_INVALID_ARG or, past an upper
+ * limit, MOE_ERR_UNSUPPORTED. */
 int moe_mx4_quantize(const void* x, void* codes, void* scales, int64_t rows, int32_t K,
                      int32_t x_type, void* stream);
 
 /* Weights as the rest of the library takes them, w [E, K, N] of w_type, to codes
  * [E, N, 16 KB] and scales [E, N, KS] for moe_mx4_product: blocks along K, rows
- * along N.  Done once, as the weights are loaded. */
+ * along N.  Done once, as the weights are loaded.  K and N below 2^31 - 256, E times K
+ * (rounded up to 256) times N (to 128) below 2^39. */
 int moe_mx4_quantize_weights(const void* w, void* codes, void* scales, int32_t E, int32_t K,
                              int32_t N, int32_t w_type, void* stream);
 
 /* The values that codes and scales stand for, to out [rows, K] of out_type
- * (exact in both types). */
+ * (exact in both types).  Limits as for moe_mx4_quantize. */
 int moe_mx4_dequantize(const void* codes, const void* scales, void* out, int64_t rows, int32_t K,
                        int32_t out_type, void* stream);
 

@@ -840,11 +840,12 @@ bool type_ok(int32_t t) { return t == MOE_BF16 || t == MOE_F32; }
 size_t type_size(int32_t t) { return t == MOE_BF16 ? 2 : 4; }
 int done() { return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP; }
 
-constexpr long long kMaxGrid = 1 << 24;   // workgroups of 256 threads: a launch's threads stay below 2^32
+constexpr long long kMaxGrid = (1 << 24) - 1;   // workgroups of 256 threads: a launch's threads stay below 2^32
+constexpr int kMaxSize = INT32_MAX - 256;        // of what is counted in 32 bits in steps of up to 256
 
 int check_rows(const void* wide, size_t wide_align, const void* codes, const void* scales, int64_t rows, int32_t K) {
   if (rows < 0 || K < 1) return MOE_ERR_INVALID_ARG;
-  if (K > INT32_MAX - 256) return MOE_ERR_UNSUPPORTED;
+  if (K > kMaxSize) return MOE_ERR_UNSUPPORTED;
   if (rows > 0 && (!wide || !codes || !scales)) return MOE_ERR_INVALID_ARG;
   if (!aligned(wide, wide_align) || !aligned(codes, 16) || !aligned(scales, 4)) return MOE_ERR_ALIGNMENT;
   return MOE_OK;
@@ -945,6 +946,7 @@ extern "C" int moe_mx4_quantize(const void* x, void* codes, void* scales, int64_
 extern "C" int moe_mx4_quantize_weights(const void* w, void* codes, void* scales, int32_t E, int32_t K, int32_t N,
                                         int32_t w_type, void* stream) {
   if (!type_ok(w_type) || E < 1 || N < 1) return MOE_ERR_INVALID_ARG;
+  if (N > kMaxSize) return MOE_ERR_UNSUPPORTED;
   const int bad = check_rows(w, type_size(w_type), codes, scales, 1, K);
   if (bad) return bad;
   const long long kt = (blocks_of(K) + kWBlocks - 1) / kWBlocks, nt = ((long long)N + kWCols - 1) / kWCols;
@@ -1039,7 +1041,7 @@ struct LayerScratch {
   size_t hc, hs, x, xc, xs, y, bytes;
 };
 bool layer_scratch(int32_t T, int32_t H, int32_t I, int32_t topk, LayerScratch* l) {
-  if (T < 0 || H < 1 || I < 1 || topk < 1 || topk > 64 || H > INT32_MAX - 256 || I > INT32_MAX - 256) return false;
+  if (T < 0 || H < 1 || I < 1 || topk < 1 || topk > 64 || H > kMaxSize || I > kMaxSize) return false;
   const size_t rows = (size_t)T * topk;
   size_t at = 0;
   auto take = [&](size_t bytes) {

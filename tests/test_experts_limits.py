@@ -113,3 +113,15 @@ def test_columns_near_2_to_31():
         assert L.moe_dispatch_rows_grad(P, P, P, 1, 1, 1, H, 0, 0, None, None) == code
         assert L.moe_combine_rows(P, P, P, P, 1, 1, 1, H, 0, 0, None, None) == code
         assert L.moe_combine_rows_grad(P, P, P, P, P, P, 1, 1, 1, H, 0, 0, None, None) == code
+
+
+def test_elements_of_the_quantisers_near_their_limits():
+    """Columns of weights past what tiles of 128 count in 32 bits, and a launch of 2^32
+    threads, which the runtime has no room for."""
+    L = X.lib()
+    for N in (2 ** 31 - 1, 2 ** 31 - 256):
+        assert L.moe_mx4_quantize_weights(P, P, P, 1, 1, N, 0, None) == B.MOE_ERR_UNSUPPORTED
+    assert L.moe_mx4_quantize_weights(P, P, P, 2 ** 24, 1, 1, 0, None) == B.MOE_ERR_UNSUPPORTED
+    for rows, K in ((2 ** 30, 32), (2 ** 20, 2 ** 15)):   # 2^35 elements, eight a thread
+        assert L.moe_mx4_quantize(P, P, P, rows, K, 0, None) == B.MOE_ERR_UNSUPPORTED
+        assert L.moe_mx4_dequantize(P, P, P, rows, K, 0, None) == B.MOE_ERR_UNSUPPORTED
