@@ -141,8 +141,9 @@ int moe_mx4_dequantize(const void* codes, const void* scales, void* out, int64_t
  *                      from expert_offsets[E] on are not written
  * Products are exact, sums are fp32, the activation is fp32, out is rounded
  * once (to nearest even).  A NaN block makes the sums it enters NaN.  Pad
- * bytes of scales are not used.  1 <= E <= 1024; a_rows >= 1 where rows > 0; the codes of a, and of one
- * expert's weights, below 2 GiB each (else MOE_ERR_UNSUPPORTED). */
+ * bytes of scales are not used.  1 <= E <= 1024; a_rows >= 1 where rows > 0; rows and K below
+ * 2^31 - 256; the codes of a, and of one expert's weights, below 2 GiB each (else
+ * MOE_ERR_UNSUPPORTED). */
 int moe_mx4_product(const void* a_codes, const void* a_scales, const void* w_codes,
                     const void* w_scales, const int32_t* expert_offsets, const int32_t* row_ids,
                     void* out, int64_t a_rows, int64_t rows, int32_t K, int32_t N, int32_t E,

@@ -1022,7 +1022,7 @@ extern "C" int moe_mx4_product(const void* a_codes, const void* a_scales, const 
                                void* stream) {
   if (a_rows < 0 || rows < 0 || K < 1 || N < 1 || E < 1 || (swiglu && N % 2)) return MOE_ERR_INVALID_ARG;
   const long long pitch = ((long long)K + kBlock - 1) / kBlock * kBlockBytes;
-  if (E > kMaxExperts || rows > INT32_MAX || pitch * N > INT32_MAX || (a_rows > 0 && pitch > INT32_MAX / a_rows))
+  if (E > kMaxExperts || rows > kMaxSize || K > kMaxSize || pitch * N > INT32_MAX || (a_rows > 0 && pitch > INT32_MAX / a_rows))
     return MOE_ERR_UNSUPPORTED;
   if (rows > 0 && (!a_codes || !a_scales || !w_codes || !w_scales || !expert_offsets || !out)) return MOE_ERR_INVALID_ARG;
   if (!aligned(a_codes, 16) || !aligned(w_codes, 16) || !aligned(a_scales, 4) || !aligned(w_scales, 4) ||
@@ -1073,7 +1073,7 @@ extern "C" int moe_mx4_layer_forward(const void* hidden, const void* w1_codes, c
                                      void* scratch, size_t scratch_bytes, void* workspace, void* stream) {
   LayerScratch l;
   if (T < 0 || H < 1 || I < 1 || E < 1 || topk < 1 || !type_ok(out_type)) return MOE_ERR_INVALID_ARG;
-  if (!layer_scratch(T, H, I, topk, &l) || I > INT32_MAX / 2 || (long long)T * topk > INT32_MAX) return MOE_ERR_UNSUPPORTED;
+  if (!layer_scratch(T, H, I, topk, &l) || I > INT32_MAX / 2 || (long long)T * topk > kMaxSize) return MOE_ERR_UNSUPPORTED;
   if (T == 0) return MOE_OK;
   // (everything is looked at before the first launch)
   if (!hidden || !w1_codes || !w1_scales || !w2_codes || !w2_scales || !expert_offsets || !token_ids || !slot_rows ||

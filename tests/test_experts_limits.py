@@ -125,3 +125,14 @@ def test_elements_of_the_quantisers_near_their_limits():
     for rows, K in ((2 ** 30, 32), (2 ** 20, 2 ** 15)):   # 2^35 elements, eight a thread
         assert L.moe_mx4_quantize(P, P, P, rows, K, 0, None) == B.MOE_ERR_UNSUPPORTED
         assert L.moe_mx4_dequantize(P, P, P, rows, K, 0, None) == B.MOE_ERR_UNSUPPORTED
+
+
+def test_rows_and_reduction_of_a_product_near_2_to_31():
+    """Rounded up to whole tiles and blocks they pass 32 bits."""
+    L = X.lib()
+
+    def product(rows=16, K=64, N=1, a_rows=1):
+        return L.moe_mx4_product(P, P, P, P, P, P, P, a_rows, rows, K, N, 1, 0, None, None)
+    for n in (2 ** 31 - 1, 2 ** 31 - 256):
+        assert product(rows=n) == product(K=n) == B.MOE_ERR_UNSUPPORTED
+    assert L.moe_mx4_layer_forward(*[P] * 10, 2 ** 31 - 256, 64, 64, 4, 1, 1, P, 1 << 60, None, None) == B.MOE_ERR_UNSUPPORTED
