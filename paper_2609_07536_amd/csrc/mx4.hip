@@ -851,15 +851,20 @@ int check_rows(const void* wide, size_t wide_align, const void* codes, const voi
   return MOE_OK;
 }
 
-// Workgroups that take several tiles: as many as are resident at once, in eight
-// equal shares (one of each XCD), and not more than there can be tiles.
+// As many tiles of bm rows as there can be, in eight equal shares (one of each XCD).
+long long most_tiles(const MxArgs& a, int bm, int nt) {
+  const long long n = a.E < a.rows ? a.E : a.rows;
+  return (((a.rows - n) / bm + n) * nt + 7) / 8 * 8;
+}
+
+// Workgroups that take several tiles: as many as are resident at once, and not more
+// than there can be tiles.
 constexpr int kCus = 256;
 template <class C>
 int launch_product(MxArgs a, bool swiglu, hipStream_t s) {
   const int bno = swiglu ? C::BN / 2 : C::BN;
   a.NT = (a.NO + bno - 1) / bno;
-  const long long n = a.E < a.rows ? a.E : a.rows;
-  const long long most = (((a.rows - n) / C::BM + n) * a.NT + 7) / 8 * 8;
+  const long long most = most_tiles(a, C::BM, a.NT);
   if (most > INT32_MAX / 2) return MOE_ERR_UNSUPPORTED;
   const unsigned grid = (unsigned)(most < C::R * kCus ? most : C::R * kCus);
   if (a.oc) mx4_product_kernel<C, true, true><<<grid, C::kThr, 0, s>>>(a);
@@ -872,11 +877,9 @@ template <class C>
 int launch_thin(MxArgs a, bool swiglu, hipStream_t s) {
   const int bno = swiglu ? C::BN / 2 : C::BN;
   a.NT = (a.NO + bno - 1) / bno;
-  const long long n = a.E < a.rows ? a.E : a.rows;
-  const long long grid = (((a.rows - n) / C::BM + n) * a.NT + 7) / 8 * 8;
-  if (grid * C::kThr >= 1ll << 32) return MOE_ERR_UNSUPPORTED;
-  if (swiglu) mx4_thin_kernel<C, true><<<(unsigned)grid, C::kThr, 0, s>>>(a);
-  else mx4_thin_kernel<C, false><<<(unsigned)grid, C::kThr, 0, s>>>(a);
+  const unsigned grid = (unsigned)most_tiles(a, C::BM, a.NT);
+  if (swiglu) mx4_thin_kernel<C, true><<<grid, C::kThr, 0, s>>>(a);
+  else mx4_thin_kernel<C, false><<<grid, C::kThr, 0, s>>>(a);
   return done();
 }
 
@@ -890,12 +893,20 @@ int launch_thin(MxArgs a, bool swiglu, hipStream_t s) {
 struct Price {
   int rows, cols;                      // of a tile, cols in rows of w
   double call, call_k, tile, tile_k;   // us, per stage of K; tiles: for one on every CU
+  int column_tiles(const MxArgs& a, bool swiglu) const {
+    const int bno = swiglu ? cols / 2 : cols;
+    return (a.NO + bno - 1) / bno;
+  }
+  // Thin kernels: a workgroup of 2 cols threads for each tile, of which a launch has less
+  // than 2^32, and sums of the experts' tiles that stay in 32 bits whatever the offsets are.
+  bool fits(const MxArgs& a, bool swiglu) const {
+    return most_tiles(a, rows, column_tiles(a, swiglu)) * 2 * cols < 1ll << 32 && (a.rows / rows + 1) * a.E <= INT32_MAX;
+  }
   double of(const MxArgs& a, bool swiglu) const {
     const double mean = (double)a.rows / a.E, hit = a.E * (1 - std::exp(-mean)), KT = (a.KB + 3) / 4;
     const double per = mean / rows + 0.5;   // ragged ends: half a tile
     const double m = std::fmin((double)a.rows, mean > 0.5 * rows ? hit * std::fmax(1.0, per) : hit);
-    const int bno = swiglu ? cols / 2 : cols;
-    return call + call_k * KT + m * ((a.NO + bno - 1) / bno) / kCus * (tile + tile_k * KT);
+    return call + call_k * KT + m * column_tiles(a, swiglu) / kCus * (tile + tile_k * KT);
   }
 };
 
@@ -904,11 +915,12 @@ int kind_of(const MxArgs& a, bool swiglu) {
   static constexpr Price kPrices[] = {{16, 32, 2.96, 0.075, 0.07, 0.0756},   {16, 32, 3.32, 0.043, 0.272, 0.0709},
                                       {32, 64, 2.94, 0.127, 0.347, 0.140},   {64, 128, 3.14, 0.216, 1.025, 0.302},
                                       {128, 128, 4.17, 0.201, 1.875, 0.310}, {256, 256, 5.61, 0.402, 8.038, 0.582}};
-  int best = 0;
-  double least = kPrices[0].of(a, swiglu);
-  for (int i = 1; i < 6; ++i) {
+  int best = 5;
+  double least = kPrices[5].of(a, swiglu);
+  for (int i = 4; i >= 0; --i) {
+    if (i < kFirstTile && !kPrices[i].fits(a, swiglu)) continue;
     const double p = kPrices[i].of(a, swiglu);
-    if (p < least) least = p, best = i;
+    if (p <= least) least = p, best = i;
   }
   return best;
 }

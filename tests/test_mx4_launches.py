@@ -36,3 +36,17 @@ result = [[product(rows, K, N, E, swiglu)[0] for swiglu in (0, 1) if swiglu == 0
             assert name.startswith(f"{mx4_shapes.KERNELS[kernel]}, {swiglu}"), (shape, names)
     for what in (mx4_shapes.REDUCTIONS, mx4_shapes.COLUMNS, mx4_shapes.EXPERTS):
         assert len(what) == len(mx4_shapes.KERNELS)
+
+
+def test_calls_too_large_for_a_thin_kernel_run_as_tiles(recorder):
+    """A thin kernel starts a workgroup for each of its tiles, and a launch has less than
+    2^32 threads; the tiles' kernels take any number."""
+    got = launch_recorder.run(recorder, _PRODUCT + """
+result = [product(rows, K, N, E, 0) for rows, K, N, E in (
+    ((1 << 30) + 5, 32, 2, 1), ((1 << 31) - 257, 32, 2, 1), ((1 << 31) - 257, 96, 33, 1000), (1 << 28, 32, 128, 1),
+    (1 << 28, 32, 2, 1024), (1 << 29, 32, 2, 1), ((1 << 25) - 32, 32, 2, 1024))]
+""")
+    for call in got[:5]:
+        assert "mx4_product_kernel" in call[0] and call[1] <= 512, call
+    for call in got[5:]:
+        assert "mx4_thin_kernel" in call[0] and call[1] * call[2] < 1 << 32, call
