@@ -269,6 +269,7 @@ struct MxArgs {
   int NO;                    // columns of out: N, or N / 2 with SwiGLU
   int OB, OS;                // their blocks and scales
   int NT;                    // tiles along them
+  int most;                  // tiles that the host counted on (launch_product)
 };
 
 // z / (1 + exp(-z)) by the reciprocal instruction (1 ulp): a full division is ten
@@ -358,11 +359,12 @@ __device__ __forceinline__ Tile unit_at(const MxArgs& a, int unit, Row row) {
     return {e0 + i, start, min(BM, __builtin_amdgcn_readlane(r1, i) - start), nt * BNO, 1};
   }
 }
-// All tiles of rows.  Offsets are clamped as in ExpertRows; bad ones are flagged.
+// All tiles.  Offsets are clamped as in ExpertRows; bad ones are flagged, and where they
+// make ranges overlap no more tiles run than there are without.
 template <int BM>
 __device__ __forceinline__ int all_tiles(const MxArgs& a) {
   const int lane = threadIdx.x & 63, cap = (int)a.rows;
-  int tiles = 0;
+  long long tiles = 0;   // of rows
   bool bad = false;
   for (int e0 = 0; e0 < a.E; e0 += 64) {
     const int e = e0 + lane, o0 = a.offsets[min(e, a.E)], o1 = a.offsets[min(e + 1, a.E)];
@@ -371,7 +373,7 @@ __device__ __forceinline__ int all_tiles(const MxArgs& a) {
   }
   if (bad && a.status && blockIdx.x == 0)
     __hip_atomic_fetch_or(a.status, kStBadRouting, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  return tiles;
+  return (int)min(tiles * a.NT, (long long)a.most);
 }
 
 // kCodes (with SwiGLU): the output, rounded to bf16 as it would be stored, leaves in 4
@@ -391,7 +393,7 @@ __global__ void __launch_bounds__(C::kThr, C::R * C::NW / 4) mx4_product_kernel(
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
   // this workgroup's tiles: every step-th of an XCD's contiguous share
-  const int units = all_tiles<C::BM>(a) * a.NT, share = (units + 7) >> 3;
+  const int units = all_tiles<C::BM>(a), share = (units + 7) >> 3;
   const int step = gridDim.x >> 3;
   int unit = (blockIdx.x & 7) * share + (blockIdx.x >> 3);
   const int last = min(((int)(blockIdx.x & 7) + 1) * share, units);
@@ -866,6 +868,7 @@ int launch_product(MxArgs a, bool swiglu, hipStream_t s) {
   a.NT = (a.NO + bno - 1) / bno;
   const long long most = most_tiles(a, C::BM, a.NT);
   if (most > INT32_MAX / 2) return MOE_ERR_UNSUPPORTED;
+  a.most = (int)most;
   const unsigned grid = (unsigned)(most < C::R * kCus ? most : C::R * kCus);
   if (a.oc) mx4_product_kernel<C, true, true><<<grid, C::kThr, 0, s>>>(a);
   else if (swiglu) mx4_product_kernel<C, true, false><<<grid, C::kThr, 0, s>>>(a);

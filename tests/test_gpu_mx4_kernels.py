@@ -189,3 +189,25 @@ def test_bad_row_ids_and_offsets(gpu_lib, kernel):
         X.mx4_product(a, w, torch.tensor(bad, dtype=torch.int32, device="cuda"), rows, row_ids=ids.clamp(min=0),
                       workspace=ws)
         assert ws.status(clear=True) == B.MOE_ERR_BAD_ROUTING, bad
+
+
+@pytest.mark.parametrize("kernel", range(6), ids=NAMES)
+def test_overlapping_experts(gpu_lib, kernel):
+    """Offsets that give most experts the same rows: flagged, no more tiles than the
+    call's rows have, nothing past `rows`, and the next call is right."""
+    import torch
+
+    from paper_2609_07536_amd import binding as B
+    from paper_2609_07536_amd import experts as X
+    E, K, N, rows = next(s for s in _of(mx4_shapes.COLUMNS, kernel) if s[2] >= 40)
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    a, w = _random((60,), K, 0, gen), _random((E, N), K, -5, gen)
+    ids = torch.randint(0, 60, (rows,), dtype=torch.int32, device="cuda", generator=gen)
+    out = torch.full((rows + 300, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    ws = B.Workspace(512)
+    for off in ([0, rows, 0, rows, 0], [0, rows, 0, rows, rows], [rows, 0, rows, 0, rows]):
+        X.mx4_product(a, w, torch.tensor(off, dtype=torch.int32, device="cuda"), rows, row_ids=ids, out=out[:rows],
+                      workspace=ws)
+        assert ws.status(clear=True) == B.MOE_ERR_BAD_ROUTING, off
+    assert bool((out[rows:] == 7).all())
+    _check(kernel, [100, 0, 60, 7], K, N, rows, False, 60)
