@@ -421,7 +421,7 @@ __global__ void __launch_bounds__(C::kThr, C::R * C::NW / 4) mx4_product_kernel(
       if (i >= t.rows_valid) return -1;
       const int id = a.row_ids ? *(const __attribute__((address_space(3))) int*)(base + C::kIds + 4 * i) : t.r0 + i;
       if (id >= 0 && id < a.a_rows) return id;
-      if (a.status) __hip_atomic_fetch_or(a.status, kStBadRouting, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (a.status && a.row_ids) __hip_atomic_fetch_or(a.status, kStBadRouting, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       return -1;
     }
     const int j = i - C::BM;

@@ -211,3 +211,26 @@ def test_overlapping_experts(gpu_lib, kernel):
         assert ws.status(clear=True) == B.MOE_ERR_BAD_ROUTING, off
     assert bool((out[rows:] == 7).all())
     _check(kernel, [100, 0, 60, 7], K, N, rows, False, 60)
+
+
+@pytest.mark.parametrize("kernel", range(6), ids=NAMES)
+def test_rows_past_the_activations_are_zeros(gpu_lib, kernel):
+    """Without row ids a row at or past a's rows is zeros, and nothing is flagged: the
+    caller's sizes say so, not the routing.  (The binding refuses such a call.)"""
+    import torch
+
+    from paper_2609_07536_amd import binding as B
+    from paper_2609_07536_amd import experts as X
+    E, K, N, rows = _of(mx4_shapes.REDUCTIONS, kernel)[-1]
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    a, w = _random((100,), K, 0, gen), _random((E, N), K, -5, gen)
+    off = torch.tensor([0, 70, 90, 290, 300], dtype=torch.int32, device="cuda")
+    out = torch.full((rows, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    ws = B.Workspace(512)
+    r = X.lib().moe_mx4_product(a.codes.data_ptr(), a.scales.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr(),
+                                off.data_ptr(), None, out.data_ptr(), 100, rows, K, N, E, 0, ws.ptr,
+                                torch.cuda.current_stream().cuda_stream)
+    assert r == 0 and ws.status() == 0
+    want, tol = _wanted(a, w, [70, 20, 10, 0], None, False)
+    assert bool(((out[:100].double() - want).abs() <= tol).all())
+    assert bool((out[100:300] == 0).all()) and bool((out[300:] == 7).all())
