@@ -48,11 +48,16 @@ class _Combine(torch.autograd.Function):
 
 def dispatch(x, routing: X.Routing):
     """x [T, H] (bf16 or fp32) to [T topk, H]: each token's row at the rows of its
-    slots, zeros at rows that no slot has."""
+    slots, zeros at rows that no slot has.  (Without a gradient x may be of any type.)"""
+    if x.dtype not in X._TYPES and x.requires_grad and torch.is_grad_enabled():
+        raise TypeError(f"x: rows of {x.dtype} can be moved but have no gradient; expected bf16 or fp32")
     return _Dispatch.apply(x, routing.slot_rows)
 
 
 def combine(y, routing: X.Routing, gates, dtype=torch.float32):
     """y [T topk, H] (bf16 or fp32) to [T, H]: the sum of each token's rows weighted
     by gates fp32 [T, topk]."""
+    rows = routing.slot_rows.numel()
+    if y.shape[0] != rows:   # (slots whose rows a shorter y lacks would be dropped)
+        raise TypeError(f"y: {y.shape[0]} rows, the routing has {rows} slots")
     return _Combine.apply(y, routing.slot_rows, gates, dtype)

@@ -85,3 +85,25 @@ def test_every_given_output_counts_as_changed(gpu_lib):
         call(out)
         assert all(t._version > v for t, v in zip(outs, was)), call
     assert [t._version for t in inputs] == before
+
+
+def test_rows_of_another_number_and_types_without_a_gradient_are_refused(gpu_lib):
+    """A y that is short of rows, and a gradient that no kernel has, when the forward pass
+    is asked for them."""
+    import torch
+
+    from paper_2609_07536_amd import autograd as A
+    from paper_2609_07536_amd import experts as X
+    ids, gates, x = _inputs()
+    r = X.sort_by_expert(ids, gates, 4)
+    y = A.dispatch(x, r)
+    for bad in (y[:-1], y[:0], torch.cat((y, y[:1]))):
+        with pytest.raises(TypeError):
+            A.combine(bad, r, gates)
+    for dtype in (torch.float16, torch.float64):
+        with pytest.raises(TypeError):
+            A.dispatch(x.to(dtype).requires_grad_(), r)
+        rows = A.dispatch(x.to(dtype), r)    # moved as they are
+        assert rows.dtype == dtype and torch.equal(rows[r.slot_rows[3, 1]], x[3].to(dtype))
+        with torch.no_grad():
+            assert torch.equal(A.dispatch(x.to(dtype).requires_grad_(), r), rows)
