@@ -107,3 +107,27 @@ def test_rows_of_another_number_and_types_without_a_gradient_are_refused(gpu_lib
         assert rows.dtype == dtype and torch.equal(rows[r.slot_rows[3, 1]], x[3].to(dtype))
         with torch.no_grad():
             assert torch.equal(A.dispatch(x.to(dtype).requires_grad_(), r), rows)
+
+
+def test_bad_slots_are_flagged_in_both_directions(gpu_lib):
+    import torch
+
+    from paper_2609_07536_amd import autograd as A
+    from paper_2609_07536_amd import binding as B
+    from paper_2609_07536_amd import experts as X
+    ids, gates, x = _inputs()
+    good = X.sort_by_expert(ids, gates, 4)
+    slots = good.slot_rows.clone()
+    slots[2, 1] = slots.numel() + 3
+    bad, ws = good._replace(slot_rows=slots), B.Workspace(512)
+    for routing, code in ((good, 0), (bad, B.MOE_ERR_BAD_ROUTING)):
+        leaf, g = x.clone().requires_grad_(), gates.clone().requires_grad_()
+        rows = A.dispatch(leaf, routing, workspace=ws)
+        assert ws.status(clear=True) == code
+        rows.sum().backward()
+        assert ws.status(clear=True) == code
+        y = rows.detach().requires_grad_()
+        out = A.combine(y, routing, g, workspace=ws)
+        assert ws.status(clear=True) == code
+        out.sum().backward()
+        assert ws.status(clear=True) == code
