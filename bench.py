@@ -40,7 +40,7 @@ PEAK_HBM_GBS = 8000.0
 # combine are read from, is the persistent kernel moe_gemm2_fused)
 KERNEL_NAME = "mixed_gemm_kernel + small_combine_kernel"
 KERNEL_SRCS = [os.path.join(ROOT, "paper_2609_07536_amd", "csrc", f)
-               for f in ("moe_gemm2.hip", "small_batch.h")]
+               for f in ("moe_gemm2.hip", "small_batch.h", "expert_units.h", "lds_loads.h", "status_bits.h")]
 TRAFFIC_FILE = os.path.join(ROOT, "profiles", "traffic_stage_dsv2lite.json")
 TICK_S = 1e-8  # the device timestamp runs at 100 MHz
 

@@ -60,3 +60,18 @@ def test_traffic_entry_follows_the_kernel_source(tmp_path, monkeypatch):
     f.write_text(json.dumps({"kernel_sha": "0" * 16, "workload": "dsv2lite",
                              "hbm_bytes_per_launch": 123}))
     assert bench.traffic_entry("dsv2lite") is None
+
+
+def test_the_kernel_source_is_every_file_that_it_includes():
+    """The traffic entry holds for the source that was measured: moe_gemm2.hip with the
+    headers of csrc/ that it includes, directly or not."""
+    import re
+    csrc = os.path.join(ROOT, "paper_2609_07536_amd", "csrc")
+    seen, todo = set(), ["moe_gemm2.hip"]
+    while todo:
+        f = todo.pop()
+        if f in seen or not os.path.exists(os.path.join(csrc, f)):   # (include/ holds the C ABI)
+            continue
+        seen.add(f)
+        todo += re.findall(r'#include "([^"]+)"', open(os.path.join(csrc, f)).read())
+    assert {os.path.basename(p) for p in bench.KERNEL_SRCS} == seen
