@@ -41,3 +41,26 @@ def test_row_ids_past_4_gib(gpu_lib):
         assert (np.abs(got - want) <= tol).all(), (r0, r1)
     del out, ids
     torch.cuda.empty_cache()
+
+
+def test_rows_of_a_large_tensor_each_in_their_place(gpu_lib):
+    """Quantised and back, 2.6e9 elements: rows on either side of 2^31 elements and the last
+    ones hold values of their own, all others zeros."""
+    import torch
+
+    from paper_2609_07536_amd import experts as X
+    rows, K = 40000, 65536
+    where = [0, 1, 7231, 7232, 32767, 32768, 32769, 39998, 39999]   # (7232 = 40000 - 2^31 / K)
+    x = torch.zeros(rows, K, dtype=torch.bfloat16, device="cuda")
+    x[where] = torch.randn(len(where), K, device="cuda", generator=torch.Generator(device="cuda").manual_seed(0)).bfloat16()
+    q = X.mx4_quantize(x)
+    codes, scales = oe.mx4_quantize(x[where].double().cpu().numpy())
+    packed = oe.mx4_pack(codes, scales)
+    assert np.array_equal(q.codes[where].cpu().numpy(), packed[0]) and np.array_equal(q.scales[where].cpu().numpy(), packed[1])
+    back = torch.full_like(x, 9.0)
+    X.mx4_dequantize(q, out=back)
+    assert np.array_equal(back[where].double().cpu().numpy(), oe.mx4_values(codes, scales))
+    back[where] = 0
+    assert not bool(back.any())
+    q.codes[where] = 0
+    assert not bool(q.codes.any())
