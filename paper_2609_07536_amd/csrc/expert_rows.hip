@@ -5,6 +5,7 @@
 #include <cstddef>
 #include <cstdint>
 
+#include "call_checks.h"
 #include "expert_units.h"
 #include "moe_experts.h"
 #include "status_bits.h"
@@ -421,11 +422,6 @@ __global__ void __launch_bounds__(256) combine_grad_kernel(const DOut* dout, con
 }
 
 // ---- host -------------------------------------------------------------------------
-
-bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
-bool type_ok(int32_t t) { return t == MOE_BF16 || t == MOE_F32; }
-size_t type_size(int32_t t) { return t == MOE_BF16 ? 2 : 4; }
-int done() { return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP; }
 
 // Workgroups of four waves, one unit a wave; past kMaxBlocks of them each wave takes several.
 constexpr long long kMaxBlocks = 1 << 20;

@@ -8,6 +8,7 @@
 #include <type_traits>
 #include <utility>
 
+#include "call_checks.h"
 #include "expert_units.h"
 #include "lds_loads.h"
 #include "moe_experts.h"
@@ -836,11 +837,6 @@ __global__ void __launch_bounds__(C::kThr) mx4_thin_kernel(MxArgs a) {
 }
 
 // ---- host --------------------------------------------------------------------------
-
-bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
-bool type_ok(int32_t t) { return t == MOE_BF16 || t == MOE_F32; }
-size_t type_size(int32_t t) { return t == MOE_BF16 ? 2 : 4; }
-int done() { return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP; }
 
 constexpr long long kMaxGrid = (1 << 24) - 1;   // workgroups of 256 threads: a launch's threads stay below 2^32
 constexpr int kMaxSize = INT32_MAX - 256;        // of what is counted in 32 bits in steps of up to 256

@@ -114,6 +114,9 @@ def _status_word(workspace):
     return workspace.ptr if workspace is not None else None
 
 
+_SORT_WITHOUT_SCRATCH = 4096   # slots, as the C ABI has it: no call to ask for small sorts
+
+
 class Routing(NamedTuple):
     """A router's choice as rows grouped by expert, as the stage and the grouped
     products take it: expert_offsets int32 [E + 1]; token_ids int32 and gate_w
@@ -145,7 +148,7 @@ def sort_by_expert(expert_ids, gates, E: int, first_expert: int = 0, out: Option
     _check(gate_w, "gate_w", (n,), _F32)
     _check(slot_rows, "slot_rows", shape, _I32)
     L, room = lib(), 0
-    if n > 4096:   # (the least that needs scratch)
+    if n > _SORT_WITHOUT_SCRATCH:
         room = L.moe_sort_scratch_size(T, topk, E)
         if scratch is None:
             scratch = _empty((room,), torch.uint8, expert_ids.device, stream)

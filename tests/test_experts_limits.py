@@ -136,3 +136,10 @@ def test_rows_and_reduction_of_a_product_near_2_to_31():
     for n in (2 ** 31 - 1, 2 ** 31 - 256):
         assert product(rows=n) == product(K=n) == B.MOE_ERR_UNSUPPORTED
     assert L.moe_mx4_layer_forward(*[P] * 10, 2 ** 31 - 256, 64, 64, 4, 1, 1, P, 1 << 60, None, None) == B.MOE_ERR_UNSUPPORTED
+
+
+def test_slots_that_a_sort_takes_without_scratch():
+    """The binding's constant is the library's."""
+    n = X._SORT_WITHOUT_SCRATCH
+    for E in (1, 32, 1024):
+        assert X.sort_scratch_size(n, 1, E) == 0 < X.sort_scratch_size(n + 1, 1, E)
