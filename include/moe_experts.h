@@ -26,7 +26,10 @@
  * as -1 and flagged: where `workspace` (a moe_gemm2 workspace of at least
  * 512 bytes, of which only the status word is used) is not NULL,
  * moe_gemm2_status reports MOE_ERR_BAD_ROUTING.  Rows that no slot has are
- * not written; a row that several slots have is written by one of them.
+ * not written; what a row that several slots have then holds is not defined (each
+ * of them writes it).  Outputs overlap neither inputs nor each other, except that
+ * combine's dy may be its y; the same address for an input of rows and the output
+ * is MOE_ERR_INVALID_ARG.
  * T, rows >= 0, 1 <= topk <= 64, 1 <= H < 2^31 - 4096 (elements; dispatch: bytes
  * of a row below 2^31), rows < 2^31, else MOE_ERR_INVALID_ARG or, past an upper
  * limit, MOE_ERR_UNSUPPORTED.

@@ -488,6 +488,7 @@ int sum_rows(bool weighted, const void* y, const int32_t* slot_rows, const float
   if (T == 0) return MOE_OK;
   if (!out || (rows > 0 && !y) || (weighted && !gates)) return MOE_ERR_INVALID_ARG;
   if (!aligned(y, type_size(y_type)) || !aligned(out, type_size(out_type)) || !aligned(gates, 4)) return MOE_ERR_ALIGNMENT;
+  if (rows > 0 && y == out) return MOE_ERR_INVALID_ARG;
   const hipStream_t s = (hipStream_t)stream;
   uint32_t* st = (uint32_t*)workspace;
 #define MOE_SUM_ROWS(In, Out)                                                                          \
@@ -603,6 +604,7 @@ extern "C" int moe_combine_rows_grad(const void* dout, const void* y, const int3
   if (!aligned(dout, type_size(dout_type)) || !aligned(y, type_size(y_type)) || !aligned(dy, type_size(y_type)) ||
       !aligned(gates, 4) || !aligned(dgates, 4))
     return MOE_ERR_ALIGNMENT;
+  if (rows > 0 && dout == dy) return MOE_ERR_INVALID_ARG;
   const hipStream_t s = (hipStream_t)stream;
   uint32_t* st = (uint32_t*)workspace;
 #define MOE_GRAD(DOut, Y) \

@@ -143,3 +143,13 @@ def test_slots_that_a_sort_takes_without_scratch():
     n = X._SORT_WITHOUT_SCRATCH
     for E in (1, 32, 1024):
         assert X.sort_scratch_size(n, 1, E) == 0 < X.sort_scratch_size(n + 1, 1, E)
+
+
+def test_an_output_in_place_of_an_input_is_refused():
+    """Other tokens' rows may still have to be read.  (combine's dy may be its y: each row
+    is read and written by its own slot's wave.)"""
+    L, Q = X.lib(), P + (1 << 16)
+    assert L.moe_dispatch_rows(P, Q, P, 4, 1, 4, 32, None, None) == B.MOE_ERR_INVALID_ARG
+    assert L.moe_dispatch_rows_grad(P, Q, P, 4, 1, 4, 32, 1, 1, None, None) == B.MOE_ERR_INVALID_ARG
+    assert L.moe_combine_rows(P, Q, Q, P, 4, 1, 4, 32, 1, 1, None, None) == B.MOE_ERR_INVALID_ARG
+    assert L.moe_combine_rows_grad(P, Q, Q, Q, P, Q, 4, 1, 4, 32, 1, 1, None, None) == B.MOE_ERR_INVALID_ARG

@@ -64,3 +64,23 @@ def test_rows_of_a_large_tensor_each_in_their_place(gpu_lib):
     assert not bool(back.any())
     q.codes[where] = 0
     assert not bool(q.codes.any())
+
+
+@pytest.mark.parametrize("H", [1, 7, 9, 511, 513, 2049, 4100])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_combine_gradient_in_place_of_its_rows(gpu_lib, H, dtype):
+    """dy written over y: the same, bit for bit, as beside it."""
+    import torch
+
+    from paper_2609_07536_amd import experts as X
+    T, k, E = 300, 3, 8
+    gen = torch.Generator(device="cuda").manual_seed(H)
+    ids = torch.randint(-1, E, (T, k), dtype=torch.int32, device="cuda", generator=gen)
+    gates = torch.randn(T, k, device="cuda", generator=gen)
+    r = X.sort_by_expert(ids, gates, E)
+    y = torch.randn(T * k, H, device="cuda", generator=gen).to(getattr(torch, dtype))
+    d = torch.randn(T, H, device="cuda", generator=gen)
+    live = int(r.expert_offsets[-1])
+    dy, dg = X.combine_rows_grad(d, y, r.slot_rows, gates)
+    got, dg2 = X.combine_rows_grad(d, y, r.slot_rows, gates, out=(y, torch.empty_like(gates)))
+    assert got is y and torch.equal(y[:live], dy[:live]) and torch.equal(dg2, dg)
