@@ -78,7 +78,7 @@ size_t moe_sort_scratch_size(int32_t T, int32_t topk, int32_t E);
  *   slot_rows       device int32 [T, topk]
  * expert_offsets, token_ids and gate_w are what moe_gemm2_combine,
  * moe_gemm1_swiglu and moe_layer_forward take with rows = T topk.
- * T >= 0, 1 <= topk <= 64, 1 <= E <= 1024, T topk < 2^31 (else
+ * T >= 0, 1 <= topk <= 64, 1 <= E <= 1024, T topk < 2^31 - 2^24 (else
  * MOE_ERR_INVALID_ARG or, past a limit, MOE_ERR_UNSUPPORTED). */
 int moe_sort_by_expert(const int32_t* expert_ids, const float* gates, int32_t* expert_offsets,
                        int32_t* token_ids, float* gate_w, int32_t* slot_rows, int32_t T,

@@ -26,10 +26,12 @@ constexpr int kMaxExperts = 1024;
 //
 // Up to kOneLaunch slots one workgroup does it all.  Beyond, a first launch
 // counts each chunk's experts and a second places the chunks, each workgroup
-// adding up all chunks' counts for itself (a few hundred KB at most, from the
-// L2): two launches without waits between workgroups.  Latency bounds both ways
-// (98304 slots move 2 MB, 0.4 us of a copy): 6 slots of 32 experts take 2.8 us of
-// GPU time, 98304 slots of 32 experts 3.0 + 6.8.
+// adding up all chunks' counts for itself, from the L2s: up to 64 KB in chunks of 512
+// and 1024 slots, at most 1 MB (256 chunks of 1024 experts) in larger ones.  Two
+// launches without waits between workgroups.  Latency bounds both ways (98304 slots
+// move 2 MB, 0.4 us of a copy): 6 slots of 32 experts take 3.0 us of GPU time, 98304
+// slots of 32 experts 3.0 + 6.9, 131072 of 256 3.0 + 13.3; with many chunks of many
+// experts the counts do: 524288 slots of 1024 experts, 256 MB of them, 5.0 + 69.
 constexpr int kOneLaunch = 4096;
 constexpr int kOneThreads = 1024;
 constexpr int kPlaceThreads = 256;

@@ -130,9 +130,9 @@ __global__ void __launch_bounds__(256) mx4_quantize_kernel(const T* x, uint8_t* 
 // w [E, K, N] to codes and scales of [E, N, K].  A workgroup takes 128 columns
 // and 256 of K: a thread's two columns over the 32 of K of a block, so a block's
 // largest magnitude needs no other lane; the codes leave through LDS as 128
-// contiguous bytes per column.  Bound by memory, with 32 loads of a thread in flight:
-// 30 experts of 704 x 2048 in bf16 (110 MB with the codes) 31.7 us, 3.5 TB/s (51.9
-// with a test before each load).
+// contiguous bytes per column.  30 experts of 704 x 2048 in bf16 (110 MB with the
+// codes) 31.5 us with 32 loads of a thread in flight (51.9 with a test before each
+// load): 3.5 TB/s, where a copy reaches 4.9.  What takes the rest is not known.
 constexpr int kWCols = 128, kWBlocks = 8;
 template <class T>
 __global__ void __launch_bounds__(256) mx4_quantize_weights_kernel(const T* w, uint8_t* codes, uint8_t* scales,
@@ -243,12 +243,15 @@ __global__ void __launch_bounds__(256) mx4_dequantize_kernel(const uint8_t* code
 // combine takes bf16.
 //
 // What bounds large calls: 98304 rows (32 experts, K 2048, N 1408 with SwiGLU, 567
-// GFLOP) 210 us, 2.7 PFLOP/s, of which the loop over K is two thirds (16 stages of
-// 256 x 256 some 26 000 clocks, the matrix instructions alone 16 400), the rest a
-// finished tile's stores and the next one's start.  That the start waits for the
+// GFLOP) 208 us, 2.7 PFLOP/s, 38% of what the instruction reaches.  The loop over K is
+// two thirds of that (16 stages of 256 x 256 some 26 000 clocks, the matrix instructions
+// alone 16 400), the rest a finished tile's stores and the next one's start.  The
+// down-projection (K 704, N 2048, 283 GFLOP, 464 MB) takes 212 us, 2.2 times its bytes
+// at a copy's rate: a tile has only six stages for its 128 KB of output, and the
+// non-temporal figures below point to the way out.  That the start waits for the
 // stores (loads and stores are counted in order) is not what costs: stores left under way
 // during the next tile's first two stages, with exact counts, gave the same outputs at
-// 196 -> 198 us here, 217 -> 213 for the down-projection (311 -> 307 with the combine).
+// 196 -> 198 us up, 217 -> 213 down (311 -> 307 with the combine).
 //
 // The stores are ordinary ones.  Non-temporal ones are faster alone (16384 tokens,
 // up 200 -> 189 us, down 226 -> 165) and slower with who reads them next (up and
@@ -685,8 +688,9 @@ __global__ void __launch_bounds__(C::kThr, C::R * C::NW / 4) mx4_product_kernel(
 // weight rows, 64 bytes of each, an instruction), while the rows of a, shared
 // by the workgroup's waves, go to LDS; no ring, one barrier per segment.
 // The 16x16x128 instruction then takes 16 weight rows and 16 rows of a.
-// Measured: 1 token (9.2 MB of weights and scales) 6.0 us, the launch and one round of
-// loads; 64 tokens (26.6 MB) 8.8 us, 3.0 TB/s.
+// Measured: 1 token (9.2 MB of weights and scales) 5.9 us: the launch, and one after
+// the other the loads of the offsets, the unit's way through memory (20 bytes of scratch
+// a lane), the row ids and the weights; 64 tokens (26.6 MB) 8.7 us, 3.0 TB/s.
 
 __device__ __forceinline__ u32x4 buffer_load16(__amdgpu_buffer_rsrc_t r, uint32_t off) {
   return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, 0));

@@ -153,3 +153,11 @@ def test_an_output_in_place_of_an_input_is_refused():
     assert L.moe_dispatch_rows_grad(P, Q, P, 4, 1, 4, 32, 1, 1, None, None) == B.MOE_ERR_INVALID_ARG
     assert L.moe_combine_rows(P, Q, Q, P, 4, 1, 4, 32, 1, 1, None, None) == B.MOE_ERR_INVALID_ARG
     assert L.moe_combine_rows_grad(P, Q, Q, Q, P, Q, 4, 1, 4, 32, 1, 1, None, None) == B.MOE_ERR_INVALID_ARG
+
+
+def test_slots_of_a_sort_near_2_to_31():
+    L = X.lib()
+    for T, k in ((2 ** 31 - 2 ** 24, 1), (2 ** 26, 32)):
+        assert L.moe_sort_by_expert(P, P, P, P, P, P, T, k, 8, 0, P, 1 << 40, None) == B.MOE_ERR_UNSUPPORTED
+        assert X.sort_scratch_size(T, k, 8) == 0
+    assert X.sort_scratch_size(2 ** 31 - 2 ** 24 - 1, 1, 8) == 256 * 8 * 4
