@@ -15,7 +15,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libmoe_gemm2.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
-SOURCES = ["selector.cpp", "moe_gemm2.hip", "expert_rows.hip", "mx4.hip"]
+SOURCES = ["selector.cpp", "moe_gemm2.hip", "expert_rows.hip", "mx4.hip",
+           "block_rows.hip", "few_tokens.hip"]
 
 # -packed-fp32-ops: keep the compiler from forming packed fp32 VALU ops.
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

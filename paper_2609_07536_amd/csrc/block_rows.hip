@@ -1,0 +1,865 @@
+// The router's choice, and the residual join with the norms on both sides, with
+// their gradients, for gfx950 (C ABI: moe_block.h).
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstddef>
+#include <cstdint>
+
+#include "call_checks.h"
+#include "moe_block.h"
+#include "status_bits.h"
+
+namespace {
+
+// ---- sums and maxima over lanes ------------------------------------------------
+//
+// Within rows of 16 lanes by data-parallel primitives (exchanges with the lane 1 and 2
+// away, then the mirrored half row and row: every lane ends up with the result), over
+// the rows of a wave by shuffles.  The order is fixed.
+template <int kCtrl>
+__device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), kCtrl, 0xf, 0xf, true));
+}
+template <int kCtrl>
+__device__ __forceinline__ int dpp(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, kCtrl, 0xf, 0xf, true);
+}
+template <int L, class T, class Op>
+__device__ __forceinline__ T over_lanes(T v, Op op) {
+  v = op(v, dpp<0xb1>(v));                     // quad_perm 1 0 3 2
+  v = op(v, dpp<0x4e>(v));                     // quad_perm 2 3 0 1
+  if (L >= 8) v = op(v, dpp<0x141>(v));        // row_half_mirror
+  if (L >= 16) v = op(v, dpp<0x140>(v));       // row_mirror
+  if (L >= 64) {
+    v = op(v, __shfl_xor(v, 16));
+    v = op(v, __shfl_xor(v, 32));
+  }
+  return v;
+}
+template <int L>
+__device__ __forceinline__ float sum_of(float v) {
+  return over_lanes<L>(v, [](float a, float b) { return a + b; });
+}
+template <int L>
+__device__ __forceinline__ float max_of(float v) {
+  return over_lanes<L>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int L>
+__device__ __forceinline__ int min_of(int v) {
+  return over_lanes<L>(v, [](int a, int b) { return min(a, b); });
+}
+
+// ---- the router's choice ---------------------------------------------------------
+//
+// L lanes take a token, R logits each in chunks of four (16 bytes of fp32): lane l
+// holds experts 4 (q L + l) + i.  A slot is the group's largest key, then the lowest
+// expert that has it; its lane notes the slot and strikes the key out.
+constexpr float kNone = -__builtin_inff();
+
+template <class T, int L, int R>
+__device__ __forceinline__ void load_logits(const T* p, int E, int l, float (&v)[R]) {
+  typedef T mem __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+#pragma unroll
+  for (int q = 0; q < R / 4; ++q) {
+    const int e = 4 * (q * L + l);
+    if (e + 4 <= E) {
+      const mem m = *(const mem*)(p + e);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[4 * q + i] = (float)m[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[4 * q + i] = e + i < E ? (float)p[e + i] : kNone;
+    }
+  }
+}
+
+__device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
+
+template <class T, int L, int R>
+__global__ void __launch_bounds__(256) choose_kernel(const T* logits, const float* bias, int32_t* ids, float* gates,
+                                                     long long first, int tokens, int E, int topk, bool softmax, bool renorm,
+                                                     float scale) {
+  const int l = threadIdx.x % L;
+  const long long t0 = first + (long long)blockIdx.x * (256 / L) + threadIdx.x / L;
+  const bool in = t0 < tokens;
+  const long long t = in ? t0 : tokens - 1;   // (groups past the last token do its work again, and write nothing)
+  float v[R], key[R], b[R];
+  load_logits<T, L, R>(logits + t * E, E, l, v);
+  if (bias) load_logits<float, L, R>(bias, E, l, b);
+  int slot[R];
+  float top = kNone;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int e = 4 * (r / 4 * L + l) + r % 4;
+    top = fmaxf(top, v[r]);
+    key[r] = bias ? v[r] + b[r] : v[r] + 0.f;   // (+ 0: equal to every comparison, -0 among them)
+    if (!(key[r] > kNone) || e >= E) key[r] = kNone;
+    slot[r] = -1;
+  }
+  int n = 0;
+  for (; n < topk; ++n) {
+    float best = key[0];
+#pragma unroll
+    for (int r = 1; r < R; ++r) best = fmaxf(best, key[r]);
+    best = max_of<L>(best);
+    if (__ballot(best > kNone) == 0) break;   // no token of the wave has another
+    int e = INT32_MAX;
+#pragma unroll
+    for (int r = R - 1; r >= 0; --r)
+      if (key[r] == best) e = 4 * (r / 4 * L + l) + r % 4;
+    e = min_of<L>(best > kNone ? e : INT32_MAX);
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (e == 4 * (r / 4 * L + l) + r % 4) {
+        slot[r] = n;
+        key[r] = kNone;
+      }
+  }
+  // p of the chosen, and what they are divided by
+  float shift = kNone, sum = 0.f, p[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    if (slot[r] >= 0) shift = fmaxf(shift, softmax || !renorm ? v[r] : fminf(v[r], 0.f));
+  shift = max_of<L>(softmax && !renorm ? top : shift);
+  int chosen = 0;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const bool on = slot[r] >= 0, all = softmax && !renorm;
+    p[r] = 0.f;
+    if (on || all) {
+      // (renormalised sigmoids by their ratio to the largest: none is lost to underflow)
+      p[r] = softmax ? expf(v[r] - shift)
+             : renorm ? expf(fminf(v[r], 0.f) - shift) / (1.f + expf(-fabsf(v[r])))
+                      : sigmoid(v[r]);
+      const int e = 4 * (r / 4 * L + l) + r % 4;
+      if (all ? e < E : on) sum += p[r];
+    }
+    chosen += on;
+  }
+  sum = sum_of<L>(sum);
+  const float f = softmax || renorm ? scale / sum : scale;
+  const int used = over_lanes<L>(chosen, [](int a, int b) { return a + b; });
+  if (!in) return;
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    if (slot[r] >= 0) {
+      ids[t * topk + slot[r]] = 4 * (r / 4 * L + l) + r % 4;
+      gates[t * topk + slot[r]] = p[r] * f;
+    }
+  for (int j = used + l; j < topk; j += L) {
+    ids[t * topk + j] = -1;
+    gates[t * topk + j] = 0.f;
+  }
+}
+
+// With q_j the gates over `scale`, the chosen slots' gradients g_j, and G = sum q_j g_j:
+//   softmax over all e     s p_e ([e chosen] g - G)
+//   renormalised softmax   s q_e (g - G), chosen e only
+//   ... sigmoid            s q_e (1 - p_e) (g - G)
+//   sigmoid                s p_e (1 - p_e) g
+// An expert that several slots name enters by its number of slots `cnt` and their sum.
+template <class T, int L, int R>
+__global__ void __launch_bounds__(256) choose_grad_kernel(const float* dgates, const T* logits, const int32_t* ids,
+                                                          T* dlogits, long long first, int tokens, int E, int topk, bool softmax,
+                                                          bool renorm, float scale, uint32_t* status) {
+  const int l = threadIdx.x % L;
+  const long long t0 = first + (long long)blockIdx.x * (256 / L) + threadIdx.x / L;
+  const bool in = t0 < tokens;
+  const long long t = in ? t0 : tokens - 1;
+  float v[R], g[R];
+  int cnt[R];
+  load_logits<T, L, R>(logits + t * E, E, l, v);
+#pragma unroll
+  for (int r = 0; r < R; ++r) g[r] = 0.f, cnt[r] = 0;
+  int some = 0;
+  for (int j = 0; j < topk; ++j) {
+    const int id = ids[t * topk + j];
+    const float d = dgates[t * topk + j];
+    if ((id < -1 || id >= E) && status)
+      __hip_atomic_fetch_or(status, kStBadRouting, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (id < 0 || id >= E) continue;
+    some = 1;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (id == 4 * (r / 4 * L + l) + r % 4) {
+        g[r] += d;
+        ++cnt[r];
+      }
+  }
+  const bool all = softmax && !renorm;
+  float shift = kNone, p[R], sum = 0.f, dot = 0.f;
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    if (all || cnt[r] > 0) shift = fmaxf(shift, softmax || !renorm ? v[r] : fminf(v[r], 0.f));
+  shift = max_of<L>(shift);
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int e = 4 * (r / 4 * L + l) + r % 4;
+    p[r] = 0.f;
+    if (all ? some && e < E : cnt[r] > 0) {
+      p[r] = softmax ? expf(v[r] - shift)
+             : renorm ? expf(fminf(v[r], 0.f) - shift) / (1.f + expf(-fabsf(v[r])))
+                      : sigmoid(v[r]);
+      sum += all ? p[r] : cnt[r] * p[r];
+    }
+  }
+  sum = sum_of<L>(sum);
+  const float inv = softmax || renorm ? (some ? 1.f / sum : 0.f) : 1.f;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    p[r] *= inv;
+    if (cnt[r] > 0) dot += p[r] * g[r];
+  }
+  dot = sum_of<L>(dot);
+  if (!in) return;
+  typedef T mem __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+#pragma unroll
+  for (int q = 0; q < R / 4; ++q) {
+    const int e = 4 * (q * L + l);
+    float d[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = 4 * q + i;
+      d[i] = 0.f;
+      if (all ? some != 0 : cnt[r] > 0) {
+        const float sg = softmax ? 1.f : sigmoid(-v[r]);   // 1 - p
+        d[i] = all      ? p[r] * (g[r] - dot)
+               : renorm ? p[r] * sg * (g[r] - cnt[r] * dot)
+                        : p[r] * sg * g[r];
+        d[i] *= scale;
+      }
+    }
+    if (e + 4 <= E) {
+      mem m;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) m[i] = (T)d[i];
+      *(mem*)(dlogits + t * E + e) = m;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (e + i < E) dlogits[t * E + e + i] = (T)d[i];
+    }
+  }
+}
+
+// ---- rows of the residual stream -----------------------------------------------------
+
+// Eight elements of a row as they lie in memory, bf16 in `a` alone: loaded together
+// whatever their types are, and converted where they are used.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x4_4 __attribute__((ext_vector_type(4), aligned(4)));
+struct Raw {
+  u32x4 a, b;
+};
+// n: how many of the eight exist (the others are zeros)
+__device__ __forceinline__ Raw load8(const void* p, bool bf16, long long at, int n) {
+  Raw r = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+  if (n >= 8) {
+    if (bf16) {
+      r.a = *(const u32x4_2*)((const uint16_t*)p + at);
+    } else {
+      r.a = *(const u32x4_4*)((const uint32_t*)p + at);
+      r.b = *(const u32x4_4*)((const uint32_t*)p + at + 4);
+    }
+  } else if (n > 0) {
+    if (bf16) {
+      const uint16_t* q = (const uint16_t*)p + at;
+#pragma unroll
+      for (int i = 0; i < 7; ++i)
+        if (i < n) r.a[i / 2] |= (uint32_t)q[i] << (16 * (i % 2));
+    } else {
+      const uint32_t* q = (const uint32_t*)p + at;
+#pragma unroll
+      for (int i = 0; i < 7; ++i)
+        if (i < n) {
+          if (i < 4) r.a[i % 4] = q[i];
+          else r.b[i % 4] = q[i];
+        }
+    }
+  }
+  return r;
+}
+__device__ __forceinline__ void floats(const Raw& r, bool bf16, float (&v)[8]) {
+  if (bf16) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(r.a[i] << 16);
+      v[2 * i + 1] = __uint_as_float(r.a[i] & 0xffff0000u);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(i < 4 ? r.a[i % 4] : r.b[i % 4]);
+  }
+}
+__device__ __forceinline__ Raw raw(const float (&v)[8], bool bf16) {
+  Raw r;
+  if (bf16) {
+    typedef __bf16 b16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const b16x2 h = {(__bf16)v[2 * i], (__bf16)v[2 * i + 1]};
+      r.a[i] = __builtin_bit_cast(uint32_t, h);
+      r.b[i] = 0;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      r.a[i] = __float_as_uint(v[i]);
+      r.b[i] = __float_as_uint(v[i + 4]);
+    }
+  }
+  return r;
+}
+__device__ __forceinline__ void store8(void* p, bool bf16, long long at, int n, const Raw& r) {
+  if (n >= 8) {
+    if (bf16) {
+      *(u32x4_2*)((uint16_t*)p + at) = r.a;
+    } else {
+      *(u32x4_4*)((uint32_t*)p + at) = r.a;
+      *(u32x4_4*)((uint32_t*)p + at + 4) = r.b;
+    }
+  } else if (n > 0) {
+#pragma unroll
+    for (int i = 0; i < 7; ++i)
+      if (i < n) {
+        if (bf16)
+          ((uint16_t*)p)[at + i] = (uint16_t)(r.a[i / 2] >> (16 * (i % 2)));
+        else
+          ((uint32_t*)p)[at + i] = i < 4 ? r.a[i % 4] : r.b[i % 4];
+      }
+  }
+}
+__device__ __forceinline__ float element(const void* p, bool bf16, long long at) {
+  return bf16 ? __uint_as_float((uint32_t)((const uint16_t*)p)[at] << 16) : ((const float*)p)[at];
+}
+
+// The random words of columns 4 block .. 4 block + 3 of a row (the multipliers and key
+// steps are the published ones).
+__device__ __forceinline__ void philox(uint32_t block, uint32_t row, uint64_t offset, uint64_t seed, uint32_t (&w)[4]) {
+  uint32_t c0 = block, c1 = row, c2 = (uint32_t)offset, c3 = (uint32_t)(offset >> 32);
+  uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
+#pragma unroll
+  for (int r = 0; r < 10; ++r) {
+    const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
+    c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+    c1 = (uint32_t)b;
+    c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+    c3 = (uint32_t)a;
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+  w[0] = c0, w[1] = c1, w[2] = c2, w[3] = c3;
+}
+
+struct JoinArgs {
+  const void *h, *y, *after, *gate, *before, *dx, *dz;   // (the gradient: h is x, the joined stream)
+  const uint64_t* rng;
+  void *x, *z, *dh, *dy;
+  float *d_after, *d_gate, *d_before, *parts;
+  int T, H;
+  bool h16, y16, z16, w16;
+  int gate_kind;
+  float scale, keep, eps;   // keep: 1 / (1 - p)
+  uint32_t least;           // least random word of a kept element
+  bool drop;
+};
+
+// v times the dropout's factor, columns c .. c + 7 of row t (c a multiple of 8)
+__device__ __forceinline__ void drop8(const JoinArgs& a, uint64_t seed, uint64_t offset, long long t, int c,
+                                      float (&v)[8]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (i % 4 == 0) philox((uint32_t)(c / 4 + i / 4), (uint32_t)t, offset, seed, w);
+    v[i] = w[i % 4] >= a.least ? v[i] * a.keep : 0.f;
+  }
+}
+
+// Sums of n values over the NT threads of a row; rows of a workgroup use LDS of their own.
+template <int NT, int n>
+__device__ __forceinline__ void row_sums(float (&v)[n], float* lds) {
+#pragma unroll
+  for (int i = 0; i < n; ++i) v[i] = sum_of<64>(v[i]);
+  if (NT == 64) return;
+  const int wave = threadIdx.x / 64;
+  __syncthreads();   // (the last sums have been read)
+  if (threadIdx.x % 64 == 0) {
+#pragma unroll
+    for (int i = 0; i < n; ++i) lds[i * (NT / 64) + wave] = v[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < n; ++i) {
+    float s = 0.f;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) s += lds[i * (NT / 64) + w];
+    v[i] = s;
+  }
+}
+
+// A workgroup takes a row, U chunks of eight columns a thread, all of it in registers:
+// every tensor is read and written once.  Bound by memory.
+template <int NT, int U>
+__global__ void __launch_bounds__(NT) join_kernel(JoinArgs a, long long first) {
+  __shared__ float lds[NT / 64];
+  const long long t = first + blockIdx.x, row = t * a.H;
+  uint64_t seed = 0, offset = 0;
+  Raw rh[U], ry[U];
+  int n[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int c = 8 * (u * NT + (int)threadIdx.x);
+    n[u] = min(8, a.H - c);
+    if (a.y) ry[u] = load8(a.y, a.y16, row + c, n[u]);
+    if (a.h) rh[u] = load8(a.h, a.h16, row + c, n[u]);
+  }
+  if (a.drop) seed = a.rng[0], offset = a.rng[1];
+  float factor = a.scale;
+  if (a.y && a.gate_kind == MOE_GATE_TOKEN) factor *= element(a.gate, a.w16, t);
+  float r = 1.f;
+  if (a.after) {
+    float s[1] = {0.f};
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float y[8];
+      floats(ry[u], a.y16, y);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[0] = fmaf(y[i], y[i], s[0]);
+    }
+    row_sums<NT>(s, lds);
+    r = rsqrtf(s[0] / a.H + a.eps);
+  }
+  float x[U][8], s[1] = {0.f};
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int c = 8 * (u * NT + (int)threadIdx.x);
+    if (a.h)
+      floats(rh[u], a.h16, x[u]);
+    else
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[u][i] = 0.f;
+    if (a.y) {
+      float v[8], w[8];
+      floats(ry[u], a.y16, v);
+      if (a.after) {
+        floats(load8(a.after, a.w16, c, n[u]), a.w16, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = v[i] * r * w[i];
+      }
+      if (a.gate_kind == MOE_GATE_CHANNEL) {
+        floats(load8(a.gate, a.w16, c, n[u]), a.w16, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= w[i];
+      }
+      if (a.drop) drop8(a, seed, offset, t, c, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[u][i] = fmaf(factor, v[i], x[u][i]);
+      const Raw o = raw(x[u], a.h16);
+      store8(a.x, a.h16, row + c, n[u], o);
+      floats(o, a.h16, x[u]);   // the norm's x is the one that is kept
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[0] = fmaf(x[u][i], x[u][i], s[0]);
+  }
+  if (!a.before) return;
+  row_sums<NT>(s, lds);
+  r = rsqrtf(s[0] / a.H + a.eps);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int c = 8 * (u * NT + (int)threadIdx.x);
+    float w[8];
+    floats(load8(a.before, a.w16, c, n[u]), a.w16, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] *= x[u][i] * r;
+    store8(a.z, a.z16, row + c, n[u], raw(w, a.z16));
+  }
+}
+
+// The gradient: with v = dz before, r the norm's factor and D = dx + r (v - x r^2
+// mean(x v)), dh = D, da = scale drop(D), db = gate da, and dy is db or, by the same
+// formula, its way back through the norm after the block.  Workgroup g takes rows g,
+// g + G, ...; its sums over rows of the columns' gradients stay in registers, go to
+// `parts` [array][G][H] and are added up by a second launch, always in the same order.
+// Bound by memory.
+template <int NT, int U>
+__global__ void __launch_bounds__(NT) join_grad_kernel(JoinArgs a) {
+  __shared__ float lds[3 * NT / 64];
+  uint64_t seed = 0, offset = 0;
+  if (a.drop) seed = a.rng[0], offset = a.rng[1];
+  const bool norm_x = a.before && a.dz, use_y = a.y && (a.after || a.gate_kind != MOE_GATE_NONE);
+  float sum_after[U][8] = {}, sum_gate[U][8] = {}, sum_before[U][8] = {};
+  for (long long t = blockIdx.x; t < a.T; t += gridDim.x) {
+    const long long row = t * a.H;
+    Raw rd[U], rx[U], rz[U], ry[U];
+    int n[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int c = 8 * (u * NT + (int)threadIdx.x);
+      n[u] = min(8, a.H - c);
+      if (norm_x) {
+        rx[u] = load8(a.h, a.h16, row + c, n[u]);
+        rz[u] = load8(a.dz, a.z16, row + c, n[u]);
+      }
+      if (use_y) ry[u] = load8(a.y, a.y16, row + c, n[u]);
+      if (a.dx) rd[u] = load8(a.dx, a.h16, row + c, n[u]);
+    }
+    float s[3] = {0.f, 0.f, 0.f};   // of x^2, x v, y^2
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int c = 8 * (u * NT + (int)threadIdx.x);
+      float v[8], w[8], x[8];
+      if (norm_x) {
+        floats(rx[u], a.h16, x);
+        floats(rz[u], a.z16, v);
+        floats(load8(a.before, a.w16, c, n[u]), a.w16, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          s[0] = fmaf(x[i], x[i], s[0]);
+          s[1] = fmaf(x[i], v[i] * w[i], s[1]);
+        }
+      }
+      if (a.after) {
+        floats(ry[u], a.y16, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[2] = fmaf(v[i], v[i], s[2]);
+      }
+    }
+    row_sums<NT>(s, lds);
+    const float r = rsqrtf(s[0] / a.H + a.eps), m = r * r * (s[1] / a.H);
+    const float q = a.after ? rsqrtf(s[2] / a.H + a.eps) : 1.f;
+    const float gate = use_y && a.gate_kind == MOE_GATE_TOKEN ? element(a.gate, a.w16, t) : 1.f;
+    float d[U][8], s2[2] = {0.f, 0.f};   // of y v of the norm after the block, and da b
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int c = 8 * (u * NT + (int)threadIdx.x);
+      float w[8];
+      if (a.dx)
+        floats(rd[u], a.h16, d[u]);
+      else
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[u][i] = 0.f;
+      if (norm_x) {
+        float x[8], z[8];
+        floats(rx[u], a.h16, x);
+        floats(rz[u], a.z16, z);
+        floats(load8(a.before, a.w16, c, n[u]), a.w16, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          d[u][i] = fmaf(r, fmaf(-m, x[i], z[i] * w[i]), d[u][i]);
+          sum_before[u][i] = fmaf(z[i], x[i] * r, sum_before[u][i]);
+        }
+      }
+      if (a.dh) store8(a.dh, a.h16, row + c, n[u], raw(d[u], a.h16));
+      if (!a.y) continue;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) d[u][i] *= a.scale;
+      if (a.drop) drop8(a, seed, offset, t, c, d[u]);
+      if (!use_y) continue;
+      float b[8], y[8], wa[8];
+      floats(ry[u], a.y16, y);
+      if (a.after) floats(load8(a.after, a.w16, c, n[u]), a.w16, wa);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) b[i] = a.after ? y[i] * q * wa[i] : y[i];
+      if (a.gate_kind == MOE_GATE_CHANNEL) {
+        floats(load8(a.gate, a.w16, c, n[u]), a.w16, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          sum_gate[u][i] = fmaf(d[u][i], b[i], sum_gate[u][i]);
+          d[u][i] *= w[i];
+        }
+      } else if (a.gate_kind == MOE_GATE_TOKEN) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          s2[1] = fmaf(d[u][i], b[i], s2[1]);
+          d[u][i] *= gate;
+        }
+      }
+      if (a.after) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          sum_after[u][i] = fmaf(d[u][i], y[i] * q, sum_after[u][i]);
+          d[u][i] *= wa[i];
+          s2[0] = fmaf(d[u][i], y[i], s2[0]);
+        }
+      }
+    }
+    if (!a.y) continue;
+    float k = 0.f;
+    if (use_y && (a.after || a.gate_kind == MOE_GATE_TOKEN)) {
+      row_sums<NT>(s2, lds);
+      if (a.gate_kind == MOE_GATE_TOKEN && a.d_gate && threadIdx.x == 0) a.d_gate[t] = s2[1];
+      k = q * q * (s2[0] / a.H);
+    }
+    if (!a.dy) continue;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int c = 8 * (u * NT + (int)threadIdx.x);
+      if (a.after) {
+        float y[8];
+        floats(ry[u], a.y16, y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[u][i] = q * fmaf(-k, y[i], d[u][i]);
+      }
+      store8(a.dy, a.y16, row + c, n[u], raw(d[u], a.y16));
+    }
+  }
+  // the columns' sums: this workgroup's part of each, or the whole where it is the only one
+  float* p = a.parts;
+  const long long part = gridDim.x > 1 ? (long long)gridDim.x * a.H : 0;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int c = 8 * (u * NT + (int)threadIdx.x), n = min(8, a.H - c);
+    const long long at = (gridDim.x > 1 ? (long long)blockIdx.x * a.H : 0) + c;
+    long long skip = 0;
+    if (a.d_after) {
+      store8(part ? (void*)(p + skip) : a.d_after, false, at, n, raw(sum_after[u], false));
+      skip += part;
+    }
+    if (a.d_gate && a.gate_kind == MOE_GATE_CHANNEL) {
+      store8(part ? (void*)(p + skip) : a.d_gate, false, at, n, raw(sum_gate[u], false));
+      skip += part;
+    }
+    if (a.d_before) store8(part ? (void*)(p + skip) : a.d_before, false, at, n, raw(sum_before[u], false));
+  }
+}
+
+// parts [array][G][H] to the arrays' sums: a workgroup takes 32 columns of an array, 32
+// threads a column.
+__global__ void __launch_bounds__(1024) column_sums_kernel(const float* parts, float* o0, float* o1, float* o2, int G,
+                                                           int H) {
+  __shared__ float lds[32][33];
+  const int c = threadIdx.x % 32, k = threadIdx.x / 32;
+  const long long col = (long long)blockIdx.x * 32 + c;
+  const float* p = parts + (long long)blockIdx.y * G * H;
+  float s = 0.f;
+  if (col < H) {
+#pragma unroll 8
+    for (int g = k; g < G; g += 32) s += p[(long long)g * H + col];
+  }
+  lds[k][c] = s;
+  __syncthreads();
+  if (k == 0 && col < H) {
+    s = 0.f;
+    for (int i = 0; i < 32; ++i) s += lds[i][c];
+    (blockIdx.y == 0 ? o0 : blockIdx.y == 1 ? o1 : o2)[col] = s;
+  }
+}
+
+// ---- host -------------------------------------------------------------------------
+
+constexpr int kMaxTopk = 64, kMaxExperts = 1024, kMaxWidth = 16384;
+
+int check_choice(const void* logits, int32_t T, int32_t E, int32_t topk, int32_t type, int32_t score) {
+  if (T < 0 || E < 1 || topk < 1 || topk > E || !type_ok(type) || (score != MOE_SOFTMAX && score != MOE_SIGMOID))
+    return MOE_ERR_INVALID_ARG;
+  if (E > kMaxExperts || topk > kMaxTopk) return MOE_ERR_UNSUPPORTED;
+  if (T > 0 && !logits) return MOE_ERR_INVALID_ARG;
+  return aligned(logits, type_size(type)) ? MOE_OK : MOE_ERR_ALIGNMENT;
+}
+
+// The lanes of a token and the logits of a lane for E experts: f(L, R) as types.
+template <int L, int R>
+struct Shape {
+  static constexpr int lanes = L, each = R;
+};
+template <class F>
+void with_shape(int E, F f) {
+  if (E <= 32) f(Shape<8, 4>());
+  else if (E <= 64) f(Shape<16, 4>());
+  else if (E <= 128) f(Shape<16, 8>());
+  else if (E <= 256) f(Shape<16, 16>());
+  else if (E <= 512) f(Shape<64, 8>());
+  else f(Shape<64, 16>());
+}
+
+// Launches of at most 2^20 workgroups (a launch holds fewer than 2^32 threads), `per` tokens
+// each: f(first token, workgroups).
+template <class F>
+void in_launches(int32_t T, int per, F f) {
+  const long long most = (long long)per << 20;
+  for (long long t = 0; t < T; t += most) f(t, (unsigned)(((T - t < most ? T - t : most) + per - 1) / per));
+}
+
+int check_join(const JoinArgs& a, int32_t T, int32_t H, int32_t h_type, int32_t y_type, int32_t z_type,
+               int32_t w_type, int32_t gate_kind, double drop) {
+  if (T < 0 || H < 1 || !type_ok(h_type) || !type_ok(y_type) || !type_ok(z_type) || !type_ok(w_type) ||
+      gate_kind < MOE_GATE_NONE || gate_kind > MOE_GATE_CHANNEL || !(drop >= 0.0 && drop < 1.0))
+    return MOE_ERR_INVALID_ARG;
+  if (H > kMaxWidth) return MOE_ERR_UNSUPPORTED;
+  if (T > 0) {   // (tensors of no rows may have no address)
+    if ((gate_kind != MOE_GATE_NONE && !a.gate) || (drop > 0.0 && !a.rng)) return MOE_ERR_INVALID_ARG;
+    if (!a.y && (a.after || gate_kind != MOE_GATE_NONE || drop > 0.0)) return MOE_ERR_INVALID_ARG;
+  }
+  const size_t h = type_size(h_type), y = type_size(y_type), z = type_size(z_type), w = type_size(w_type);
+  if (!aligned(a.h, h) || !aligned(a.x, h) || !aligned(a.dx, h) || !aligned(a.dh, h) || !aligned(a.y, y) ||
+      !aligned(a.dy, y) || !aligned(a.z, z) || !aligned(a.dz, z) || !aligned(a.after, w) || !aligned(a.gate, w) ||
+      !aligned(a.before, w) || !aligned(a.rng, 8) || !aligned(a.d_after, 4) || !aligned(a.d_gate, 4) ||
+      !aligned(a.d_before, 4))
+    return MOE_ERR_ALIGNMENT;
+  return MOE_OK;
+}
+void set_common(JoinArgs* a, int32_t T, int32_t H, int32_t h_type, int32_t y_type, int32_t z_type, int32_t w_type,
+                int32_t gate_kind, float scale, double drop, float eps) {
+  a->T = T, a->H = H;
+  a->h16 = h_type == MOE_BF16, a->y16 = y_type == MOE_BF16, a->z16 = z_type == MOE_BF16, a->w16 = w_type == MOE_BF16;
+  a->gate_kind = gate_kind;
+  a->scale = scale, a->eps = eps;
+  a->drop = drop > 0.0;
+  a->keep = (float)(1.0 / (1.0 - drop));
+  a->least = (uint32_t)std::floor(drop * 4294967296.0);
+}
+bool same(const void* p, const void* q) { return p && p == q; }
+
+// Threads of a row and chunks of a thread: f(NT, U) as types (Shape).
+template <class F>
+void with_row(int H, F f) {
+  if (H <= 512) f(Shape<64, 1>());
+  else if (H <= 2048) f(Shape<256, 1>());
+  else if (H <= 8192) f(Shape<1024, 1>());
+  else f(Shape<1024, 2>());
+}
+// Workgroups of the gradient: enough to fill the card, few enough that their parts are
+// small beside the rows.
+int grad_groups(int T, int H) {
+  const int most = H <= 512 ? 4096 : H <= 2048 ? 1024 : 256;
+  return T < most ? (T < 1 ? 1 : T) : most;
+}
+
+}  // namespace
+
+extern "C" int moe_choose(const void* logits, const float* bias, int32_t* ids, float* gates, int32_t T, int32_t E,
+                          int32_t topk, int32_t logits_type, int32_t score, int32_t renormalize, float scale,
+                          void* stream) {
+  const int bad = check_choice(logits, T, E, topk, logits_type, score);
+  if (bad) return bad;
+  if (T == 0) return MOE_OK;
+  if (!ids || !gates) return MOE_ERR_INVALID_ARG;
+  if (!aligned(bias, 4) || !aligned(ids, 4) || !aligned(gates, 4)) return MOE_ERR_ALIGNMENT;
+  if (logits == (const void*)ids || logits == (const void*)gates || (void*)ids == (void*)gates || bias == gates ||
+      same(bias, ids))
+    return MOE_ERR_INVALID_ARG;
+  const hipStream_t s = (hipStream_t)stream;
+  with_shape(E, [&](auto shape) {
+    constexpr int L = decltype(shape)::lanes, R = decltype(shape)::each, per = 256 / L;
+    in_launches(T, per, [&](long long first, unsigned blocks) {
+      if (logits_type == MOE_BF16)
+        choose_kernel<__bf16, L, R><<<blocks, 256, 0, s>>>((const __bf16*)logits, bias, ids, gates, first, T, E, topk,
+                                                           score == MOE_SOFTMAX, renormalize != 0, scale);
+      else
+        choose_kernel<float, L, R><<<blocks, 256, 0, s>>>((const float*)logits, bias, ids, gates, first, T, E, topk,
+                                                          score == MOE_SOFTMAX, renormalize != 0, scale);
+    });
+  });
+  return done();
+}
+
+extern "C" int moe_choose_grad(const float* dgates, const void* logits, const int32_t* ids, void* dlogits, int32_t T,
+                               int32_t E, int32_t topk, int32_t logits_type, int32_t score, int32_t renormalize,
+                               float scale, void* workspace, void* stream) {
+  const int bad = check_choice(logits, T, E, topk, logits_type, score);
+  if (bad) return bad;
+  if (T == 0) return MOE_OK;
+  if (!dgates || !ids || !dlogits) return MOE_ERR_INVALID_ARG;
+  if (!aligned(dgates, 4) || !aligned(ids, 4) || !aligned(dlogits, type_size(logits_type)) || !aligned(workspace, 256))
+    return MOE_ERR_ALIGNMENT;
+  if (dlogits == logits || dlogits == (const void*)dgates || dlogits == (const void*)ids) return MOE_ERR_INVALID_ARG;
+  const hipStream_t s = (hipStream_t)stream;
+  uint32_t* st = (uint32_t*)workspace;
+  with_shape(E, [&](auto shape) {
+    constexpr int L = decltype(shape)::lanes, R = decltype(shape)::each, per = 256 / L;
+    in_launches(T, per, [&](long long first, unsigned blocks) {
+      if (logits_type == MOE_BF16)
+        choose_grad_kernel<__bf16, L, R><<<blocks, 256, 0, s>>>(dgates, (const __bf16*)logits, ids, (__bf16*)dlogits,
+                                                                first, T, E, topk, score == MOE_SOFTMAX,
+                                                                renormalize != 0, scale, st);
+      else
+        choose_grad_kernel<float, L, R><<<blocks, 256, 0, s>>>(dgates, (const float*)logits, ids, (float*)dlogits,
+                                                               first, T, E, topk, score == MOE_SOFTMAX,
+                                                               renormalize != 0, scale, st);
+    });
+  });
+  return done();
+}
+
+extern "C" int moe_join(const void* h, const void* y, const void* after, const void* gate, const void* before,
+                        const uint64_t* rng, void* x, void* z, int32_t T, int32_t H, int32_t h_type, int32_t y_type,
+                        int32_t z_type, int32_t w_type, int32_t gate_kind, float scale, double drop, float eps,
+                        void* stream) {
+  JoinArgs a = {};
+  a.h = h, a.y = y, a.after = after, a.gate = gate, a.before = before, a.rng = rng, a.x = x, a.z = z;
+  const int bad = check_join(a, T, H, h_type, y_type, z_type, w_type, gate_kind, drop);
+  if (bad) return bad;
+  if (T == 0) return MOE_OK;
+  if ((!h && !y) || (y && !x) || (before && !z) || (!y && !before)) return MOE_ERR_INVALID_ARG;
+  if (!y) a.x = nullptr;
+  if (!before) a.z = nullptr;
+  for (const void* in : {h, y, after, gate, before, (const void*)rng})
+    if (same(a.z, in) || (in != h && same(a.x, in))) return MOE_ERR_INVALID_ARG;
+  if (same(a.x, a.z) || (same(a.x, h) && h == y)) return MOE_ERR_INVALID_ARG;
+  set_common(&a, T, H, h_type, y_type, z_type, w_type, gate_kind, scale, drop, eps);
+  const hipStream_t s = (hipStream_t)stream;
+  with_row(H, [&](auto shape) {
+    constexpr int NT = decltype(shape)::lanes, U = decltype(shape)::each;
+    in_launches(T, 1, [&](long long first, unsigned blocks) { join_kernel<NT, U><<<blocks, NT, 0, s>>>(a, first); });
+  });
+  return done();
+}
+
+extern "C" size_t moe_join_grad_scratch_size(int32_t T, int32_t H) {
+  if (T < 0 || H < 1 || H > kMaxWidth) return 0;
+  const int G = grad_groups(T, H);
+  return G > 1 ? (size_t)G * H * 3 * sizeof(float) : 0;
+}
+
+extern "C" int moe_join_grad(const void* dx, const void* dz, const void* x, const void* y, const void* after,
+                             const void* gate, const void* before, const uint64_t* rng, void* dh, void* dy,
+                             float* d_after, float* d_gate, float* d_before, int32_t T, int32_t H, int32_t h_type,
+                             int32_t y_type, int32_t z_type, int32_t w_type, int32_t gate_kind, float scale,
+                             double drop, float eps, void* scratch, size_t scratch_bytes, void* stream) {
+  JoinArgs a = {};
+  a.dx = dx, a.dz = dz, a.h = x, a.y = y, a.after = after, a.gate = gate, a.before = before, a.rng = rng;
+  a.dh = dh, a.dy = dy, a.d_after = d_after, a.d_gate = d_gate, a.d_before = d_before;
+  const int bad = check_join(a, T, H, h_type, y_type, z_type, w_type, gate_kind, drop);
+  if (bad) return bad;
+  if ((d_after && !after) || (d_before && !before) || (d_gate && gate_kind == MOE_GATE_NONE)) return MOE_ERR_INVALID_ARG;
+  if (T > 0 && ((!dx && !dz) || (dz && (!before || !x)) || (dy && !y))) return MOE_ERR_INVALID_ARG;
+  for (const void* o : {(const void*)dh, (const void*)dy, (const void*)d_after, (const void*)d_gate, (const void*)d_before})
+    for (const void* in : {dx, dz, x, y, after, gate, before, (const void*)rng})
+      if (same(o, in) && !(o == dh && in == dx)) return MOE_ERR_INVALID_ARG;
+  if (same(dh, dx) && dx == dz) return MOE_ERR_INVALID_ARG;
+  const void* outs[5] = {dh, dy, d_after, d_gate, d_before};
+  for (int i = 0; i < 5; ++i)
+    for (int j = 0; j < i; ++j)
+      if (same(outs[i], outs[j])) return MOE_ERR_INVALID_ARG;
+  set_common(&a, T, H, h_type, y_type, z_type, w_type, gate_kind, scale, drop, eps);
+  const int G = grad_groups(T, H);
+  const bool channel = gate_kind == MOE_GATE_CHANNEL && d_gate;
+  const int arrays = (d_after != nullptr) + channel + (d_before != nullptr);
+  if (T == 0 && arrays == 0) return MOE_OK;
+  if (G > 1 && arrays > 0) {
+    if (!scratch || scratch_bytes < moe_join_grad_scratch_size(T, H)) return MOE_ERR_WORKSPACE;
+    if (!aligned(scratch, 16)) return MOE_ERR_ALIGNMENT;
+    a.parts = (float*)scratch;
+  }
+  if (T == 0) a.drop = false;
+  const hipStream_t s = (hipStream_t)stream;
+  with_row(H, [&](auto shape) {
+    constexpr int NT = decltype(shape)::lanes, U = decltype(shape)::each;
+    join_grad_kernel<NT, U><<<(unsigned)G, NT, 0, s>>>(a);
+  });
+  if (G > 1 && arrays > 0) {
+    if (hipGetLastError() != hipSuccess) return MOE_ERR_HIP;
+    float* o[3] = {nullptr, nullptr, nullptr};
+    int n = 0;
+    if (d_after) o[n++] = d_after;
+    if (channel) o[n++] = d_gate;
+    if (d_before) o[n++] = d_before;
+    column_sums_kernel<<<dim3((unsigned)((H + 31) / 32), (unsigned)arrays), 1024, 0, s>>>(a.parts, o[0], o[1], o[2], G,
+                                                                                          H);
+  }
+  return done();
+}
+
+extern "C" int moe_block_abi_version(void) { return 100; }
