@@ -42,7 +42,7 @@ def lib() -> ctypes.CDLL:
         L.moe_join.argtypes = [vp] * 8 + [i32] * 7 + [f32, ctypes.c_double, f32, vp]
         L.moe_join_grad_scratch_size.argtypes = [i32] * 2
         L.moe_join_grad.argtypes = [vp] * 13 + [i32] * 7 + [f32, ctypes.c_double, f32, vp, sz, vp]
-        L.moe_few_scratch_size.argtypes = [i32] * 3
+        L.moe_few_scratch_size.argtypes = [i32] * 5
         L.moe_few_forward.argtypes = [vp] * 6 + [i32] * 7 + [vp, sz, vp]
         L.moe_few_forward_mx4.argtypes = [vp] * 8 + [i32] * 7 + [vp, sz, vp]
         for name in EXPORTED:
@@ -289,8 +289,8 @@ def join_grad(d_h, d_z, h, y=None, after=None, gate=None, scale: float = 1.0, dr
 
 # ---- the post-router layer for a few tokens --------------------------------------------------
 
-def layer_few_scratch_size(T: int, I: int, topk: int) -> int:
-    return 0 if max(T, I, topk) > _MOST else int(lib().moe_few_scratch_size(T, I, topk))
+def layer_few_scratch_size(T: int, H: int, I: int, E: int, topk: int) -> int:
+    return 0 if max(T, H, I, E, topk) > _MOST else int(lib().moe_few_scratch_size(T, H, I, E, topk))
 
 
 def layer_few(hidden, w1, w2, expert_ids, gates, first_expert: int = 0, out=None, dtype=torch.float32, scratch=None,
@@ -333,7 +333,7 @@ def layer_few(hidden, w1, w2, expert_ids, gates, first_expert: int = 0, out=None
     _check(out, "out", (T, H), _FLOAT)
     L = lib()
     if scratch is None:
-        scratch = _empty((L.moe_few_scratch_size(T, I, topk),), torch.uint8, hidden.device, stream)
+        scratch = _empty((L.moe_few_scratch_size(T, H, I, E, topk),), torch.uint8, hidden.device, stream)
     _check(scratch, "scratch", scratch.shape, _U8)
     rest = (expert_ids.data_ptr(), gates.data_ptr(), out.data_ptr(), T, H, I, E, topk, first_expert, _TYPES[out.dtype],
             scratch.data_ptr(), scratch.numel(),

@@ -10,33 +10,30 @@
 #include <cstdint>
 
 #include "call_checks.h"
+#include "lds_loads.h"
 #include "moe_block.h"
 
 namespace {
 
 constexpr int kMaxTopk = 64, kMaxExperts = 1024;
-constexpr int kMaxSlots = MOE_FEW_TOKENS * kMaxTopk;
 constexpr int kMaxWidth = 1 << 22;   // H and I
+constexpr int kMaxShares = 8;        // workgroups that share a tile of the second launch
 constexpr int kBlock = 32;   // elements of an mx4 block
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4_2 __attribute__((ext_vector_type(4), aligned(2)));
 
-// What the first launch leaves for the second: the hit experts in the order of their
-// first slots, and for each token that names one the row of its activation (the first of
-// its slots that does) and the sum of their gates, in slot order.
+// What the first launch leaves for the second of a unit (a slot that is the first to name
+// its expert, or an expert where there are more slots than experts): the expert or -1, the
+// tokens that name it and the sum of each one's gates, in slot order.  The activation of
+// token t for it is row T unit + t.
 struct Hit {
-  int32_t e, pad[3];
-  int32_t row[MOE_FEW_TOKENS];   // or -1
+  int32_t e;
+  uint32_t tokens;
   float gate[MOE_FEW_TOKENS];
-};
-struct Plan {
-  int32_t n, pad[15];
-  Hit hit[1];
 };
 
 struct FewArgs {
@@ -45,10 +42,12 @@ struct FewArgs {
   const int32_t* ids;
   const float* gates;
   void* out;
-  Plan* plan;
-  __bf16* act;   // [slots][pitch]
-  int T, H, I, E, topk, first, slots, pitch;
-  int tiles;     // of an expert's columns (first launch)
+  Hit* hits;         // [units]
+  __bf16* act;       // [T units][pitch]
+  float* parts;      // [shares][T][H], where the second launch has several shares
+  uint32_t* count;   // [tiles of the second launch]: shares that are there
+  int T, H, I, E, topk, first, slots, units, pitch;
+  int tiles, out_tiles, shares;   // (tiles: of a unit of the first launch)
   bool out16;
 };
 
@@ -58,9 +57,123 @@ __device__ __forceinline__ int expert_of(const FewArgs& a, int id) {
 }
 
 // ---- operands ----------------------------------------------------------------------
+//
+// Weights come by buffer loads: past an expert's last row they read zeros, so no step
+// needs a test.  Offsets are below 2^31; kOutOfRange is past every extent.
+typedef __amdgpu_buffer_rsrc_t Buffer;
+__device__ __forceinline__ Buffer buffer(const void* p, long long bytes) {
+  const uint64_t b = (uint64_t)(uintptr_t)p;
+  const uint64_t u = ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(b >> 32)) << 32) |
+                     (uint32_t)__builtin_amdgcn_readfirstlane((int)b);
+  return __builtin_amdgcn_make_buffer_rsrc((void*)(uintptr_t)u, 0, __builtin_amdgcn_readfirstlane((int)bytes),
+                                           0x00020000);   // (raw 32-bit data)
+}
+__device__ __forceinline__ u32x4 load16(Buffer b, uint32_t at) { return __builtin_amdgcn_raw_buffer_load_b128(b, at, 0, 0); }
 
-// Eight elements of a row from k on, zeros past its end.
-__device__ __forceinline__ bf16x8 row8(const __bf16* row, int k, int K) {
+__device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// bf16 weights, [K, columns]: a lane takes four neighbouring columns of eight rows of K, so
+// that sixteen lanes read whole 128-byte lines, and eight elements of a token's row.  The
+// matrix instruction takes a column's eight values: one permutation for two of them.
+struct Bf16Step {
+  u32x2 w[8];
+  u32x4 x;
+  __device__ __forceinline__ void load(Buffer b, uint32_t at, uint32_t pitch) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = __builtin_amdgcn_raw_buffer_load_b64(b, at + i * pitch, 0, 0);
+  }
+  __device__ __forceinline__ u32x4 column(int c) const {
+    u32x4 v;
+#pragma unroll
+    for (int p = 0; p < 4; ++p)
+      v[p] = __builtin_amdgcn_perm(w[2 * p + 1][c / 2], w[2 * p][c / 2], c % 2 ? 0x07060302u : 0x05040100u);
+    return v;
+  }
+};
+// A wave's n steps, the loads of two of them under way; a step past the end is loads of
+// nothing and products of zeros, without a branch, so that the waits stay exact.
+template <class Load, class Use>
+__device__ __forceinline__ void run_steps(int n, Load load, Use use) {
+  Bf16Step b[2];
+  load(b[0], 0);
+  load(b[1], 1);
+  int i = 0;
+  for (; i + 2 < n; i += 2) {
+    use(b[0], i);
+    load(b[0], i + 2);
+    use(b[1], i + 1);
+    load(b[1], i + 3);
+  }
+  use(b[0], i);
+  use(b[1], i + 1);
+}
+
+// Weights in mx4, N rows of codes along K: a wave's step is 16 blocks (512 of K), a lane's
+// four of them of each row.  The scales of a row's 16 blocks come by one load and the
+// tokens' elements through LDS, a row of them by one load: four loads of elements for every
+// load of codes, most of them of tokens that do not name the expert, and one of a scale
+// byte took half of the time (46 MB in 18.4 us, 10.9 without them).
+constexpr int kStepBlocks = 16, kStepK = kStepBlocks * kBlock;
+constexpr int kStepBytes = 2 * kStepK + 16;   // of a token's row in LDS (rows start four banks apart)
+template <int N>
+struct Mx4Step {
+  u32x4 codes[N][4], scale[N];
+  // row r of KB blocks and KS scale bytes, from block kb0 on
+  __device__ __forceinline__ void load(int n, Buffer c, Buffer s, uint32_t r, int kb0, int KB, int KS, bool in) {
+    const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int kb = kb0 + 4 * j + g;
+      codes[n][j] = load16(c, in && kb < KB ? (r * KB + kb) * 16 : kOutOfRange);
+    }
+    if (KS >= kStepBlocks) {   // (the last 16 bytes of the row at most)
+      scale[n] = load16(s, in ? r * KS + min(kb0, KS - kStepBlocks) : kOutOfRange);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        scale[n][j] = __builtin_amdgcn_raw_buffer_load_b32(s, in && 4 * j < KS ? r * KS + 4 * j : kOutOfRange, 0, 0);
+    }
+  }
+  // brings the scales of blocks kb0 + 4 j .. into scale[n][j]
+  __device__ __forceinline__ void align(int kb0, int KS) {
+    for (int past = kb0 + kStepBlocks - KS; KS >= kStepBlocks && past > 0; past -= 4)
+#pragma unroll
+      for (int n = 0; n < N; ++n) scale[n] = u32x4{scale[n][1], scale[n][2], scale[n][3], 0};
+  }
+  __device__ __forceinline__ uint32_t byte(int n, int j) const {
+    return (scale[n][j] >> (((threadIdx.x & 63) >> 4) * 8)) & 255;
+  }
+  // eight values (what a code stands for is exact in bf16)
+  __device__ __forceinline__ u32x4 eight(int n, int j, int q) const {
+    const uint32_t b = byte(n, j);
+    const float s = __uint_as_float(b == 0 ? 0x00400000u : b << 23);
+    const uint32_t c = codes[n][j][q];
+    return {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0)),
+            __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1)),
+            __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2)),
+            __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3))};
+  }
+  // whether one of the lane's blocks is NaN
+  __device__ __forceinline__ bool bad(int n, int kb0, int KB) const {
+    bool r = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r |= byte(n, j) == 255 && kb0 + 4 * j + (int)((threadIdx.x & 63) >> 4) < KB;
+    return r;
+  }
+};
+// v, or NaN where a lane of the same column had a NaN block (its 32 operands are anything).
+__device__ __forceinline__ f32x4 with_nan(f32x4 v, bool bad) {
+  const uint64_t m = __ballot(bad);
+  if (m) {   // (uniform, and rare)
+    if ((m >> (threadIdx.x & 15)) & 0x0001000100010001ull) v = f32x4{1.f, 1.f, 1.f, 1.f} * __builtin_nanf("");
+  }
+  return v;
+}
+
+// Eight elements of a row of K from k on, zeros past its end, for any K.
+__device__ __forceinline__ u32x4 row8(const __bf16* row, int k, int K) {
   u32x4 v = {0, 0, 0, 0};
   if (k + 8 <= K) {
     v = *(const u32x4_2*)(row + k);
@@ -70,359 +183,444 @@ __device__ __forceinline__ bf16x8 row8(const __bf16* row, int k, int K) {
     for (int i = 0; i < 7; ++i)
       if (k + i < K) v[i / 2] |= (uint32_t)q[i] << (16 * (i % 2));
   }
-  return __builtin_bit_cast(bf16x8, v);
+  return v;
 }
-
-// C neighbouring columns of a row of bf16 weights.
-template <int C>
-struct Cols {
-  uint32_t d[C / 2];
-};
-template <int C>
-__device__ __forceinline__ Cols<C> load_cols(const __bf16* p) {
-  Cols<C> r;
-  if constexpr (C == 8) {
-    const u32x4 v = *(const u32x4*)p;
-    r.d[0] = v[0], r.d[1] = v[1], r.d[2] = v[2], r.d[3] = v[3];
-  } else if constexpr (C == 4) {
-    const u32x2 v = *(const u32x2*)p;
-    r.d[0] = v[0], r.d[1] = v[1];
-  } else {
-    r.d[0] = *(const uint32_t*)p;
+// 512 elements from k on of the rows (of K, `pitch` apart) of the tokens in the mask to the
+// wave's LDS, zeros past their end.  The rows of other tokens hold anything: they make
+// results of these tokens only, which nobody takes.  kOdd: K is no multiple of 32.
+template <bool kOdd>
+__device__ __forceinline__ void rows_to_lds(uint8_t* lds, const __bf16* x, int T, int pitch, uint32_t tokens, int k, int K) {
+  const int lane = threadIdx.x & 63;
+  k += 8 * lane;
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (what was there has been read)
+  const i32x4 r = buffer_rsrc(x, 2LL * T * pitch);
+  for (uint32_t m = tokens; m; m &= m - 1) {
+    const int t = __builtin_ctz(m);
+    if constexpr (kOdd)
+      *(u32x4*)(lds + t * kStepBytes + 16 * lane) = row8(x + (long long)t * pitch, k, K);
+    else
+      dma16(r, k < K ? 2u * (t * pitch + k) : kOutOfRange, lds_addr(lds + t * kStepBytes));
   }
-  return r;
 }
-
-// Where a lane's part of the products lies: with D > 1, the 16 rows are D times 16 / D
-// tokens and the 16 columns D times 16 / D columns, each time another 32 of K: the D blocks
-// on the diagonal are products (their sum is the result), the others are not used.
-template <int D>
-struct Lane {
-  static constexpr int tokens = 16 / D;
-  int l, g, at, part;   // lane, group of 8 of K, token (A) or column (B), diagonal block
-  __device__ __forceinline__ Lane() {
-    l = threadIdx.x & 63;
-    g = l >> 4;
-    at = l & (tokens - 1);
-    part = (l & 15) / tokens;
-  }
-};
-
-// Eight rows of K by C columns of bf16 weights, and what the matrix instruction takes of
-// them: a column's eight values, by one permutation for two of them.
-template <int C>
-struct Weights {
-  Cols<C> r[8];
-  __device__ __forceinline__ void load(const __bf16* w, long long pitch, bool in) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (in) {
-        r[i] = load_cols<C>(w + i * pitch);
-      } else {
-#pragma unroll
-        for (int j = 0; j < C / 2; ++j) r[i].d[j] = 0;
-      }
-    }
-  }
-  __device__ __forceinline__ bf16x8 column(int c) const {
-    u32x4 v;
-#pragma unroll
-    for (int p = 0; p < 4; ++p)
-      v[p] = __builtin_amdgcn_perm(r[2 * p + 1].d[c / 2], r[2 * p].d[c / 2], c % 2 ? 0x07060302u : 0x05040100u);
-    return __builtin_bit_cast(bf16x8, v);
-  }
-};
-
-// A block of 32 mx4 values as four operands of eight (what a code stands for is exact in
-// bf16).
-struct Block {
-  u32x4 codes;
-  uint32_t byte;
-  __device__ __forceinline__ void load(const uint8_t* c, const uint8_t* s, bool in) {
-    codes = {0, 0, 0, 0};
-    byte = 0;
-    if (in) {
-      codes = *(const u32x4*)c;
-      byte = *s;
-    }
-  }
-  __device__ __forceinline__ bf16x8 eight(int q) const {
-    const float s = __uint_as_float(byte == 0 ? 0x00400000u : byte << 23);
-    const bf16x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[q], s, 0),
-                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[q], s, 1),
-                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[q], s, 2),
-                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[q], s, 3)};
-    u32x4 v;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = byte == 255 ? 0x7fc07fc0u : __builtin_bit_cast(uint32_t, p[i]);
-    return __builtin_bit_cast(bf16x8, v);
-  }
-};
-
-__device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+// The four operands of eight of block 4 j + g of the lane's token.
+__device__ __forceinline__ u32x4 row_operand(const uint8_t* lds, int t, int j, int q) {
+  return *(const u32x4*)(lds + t * kStepBytes + (4 * j + (int)((threadIdx.x & 63) >> 4)) * 2 * kBlock + 16 * q);
 }
 
 // ---- the first launch ------------------------------------------------------------------
 
-// The plan, by the launch's last workgroup.
-__device__ void make_plan(const FewArgs& a) {
-  __shared__ int32_t ids[kMaxSlots], index[kMaxExperts];
-  __shared__ float gates[kMaxSlots];
-  __shared__ int n;
-  const int tid = threadIdx.x, threads = blockDim.x;
-  for (int e = tid; e < a.E; e += threads) index[e] = INT32_MAX;
-  for (int s = tid; s < a.slots; s += threads) {
-    ids[s] = expert_of(a, a.ids[s]);
-    gates[s] = a.gates[s];
-  }
-  __syncthreads();
-  for (int s = tid; s < a.slots; s += threads)
-    if (ids[s] >= 0) atomicMin(&index[ids[s]], s);
-  __syncthreads();
-  if (tid < 64) {   // the experts in the order of their first slots
-    int at = 0;
-    for (int s0 = 0; s0 < a.slots; s0 += 64) {
-      const int s = s0 + tid, e = s < a.slots ? ids[s] : -1;
-      const bool leads = e >= 0 && index[e] == s;
-      const uint64_t m = __ballot(leads);
-      if (leads) a.plan->hit[at + __popcll(m & ((1ull << tid) - 1))].e = e;
-      at += __popcll(m);
-    }
-    if (tid == 0) a.plan->n = n = at;
-  }
-  __syncthreads();
-  // (a leader's place again, by counting, where its token's rows and gates are filled in)
-  for (int i = tid; i < n * MOE_FEW_TOKENS; i += threads) {
-    Hit* h = &a.plan->hit[i / MOE_FEW_TOKENS];
-    const int t = i % MOE_FEW_TOKENS, e = h->e;
-    int row = -1;
-    float g = 0.f;
-    if (t < a.T)
-      for (int j = 0; j < a.topk; ++j)
-        if (ids[t * a.topk + j] == e) {
-          row = row < 0 ? t * a.topk + j : row;
-          g += gates[t * a.topk + j];
-        }
-    h->row[t] = row;
-    h->gate[t] = g;
-  }
-}
-
-// A workgroup's expert and tile; the rows of the activation that its tokens have in
-// it (lane t of each wave; -1: not this expert's).  False: nothing to do.
-__device__ __forceinline__ bool few_unit(const FewArgs& a, int* e, int* tile, int* row) {
-  const int lane = threadIdx.x & 63;
-  const int u = blockIdx.x / a.tiles;
-  *tile = blockIdx.x - u * a.tiles;
+// A workgroup's expert and the tokens that name it (bit t); false: nothing to do.  Lane t
+// looks through token t's slots; the loads of eight are under way together, and wait for
+// nothing.
+__device__ __forceinline__ bool few_unit(const FewArgs& a, int u, int* e, uint32_t* tokens) {
+  const int t = threadIdx.x & 63;
   const bool by_slot = a.slots <= a.E;
-  *e = by_slot ? expert_of(a, a.ids[u]) : u;
-  if (*e < 0) return false;
-  if (by_slot) {   // the first slot that names the expert has it
-    bool other = false;
-    for (int s = lane; s < u; s += 64) other |= expert_of(a, a.ids[s]) == *e;
-    if (__ballot(other)) return false;
+  const int32_t* p = a.ids + min(t, a.T - 1) * a.topk;
+  const int own = a.ids[by_slot ? u : 0];
+  int at = -1;   // token t's first slot that names the expert
+  *e = 0;
+  for (int j0 = 0; j0 < a.topk; j0 += 8) {
+    int id[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) id[i] = p[min(j0 + i, a.topk - 1)];
+    *e = by_slot ? expert_of(a, own) : u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (at < 0 && j0 + i < a.topk && expert_of(a, id[i]) == *e) at = t * a.topk + j0 + i;
   }
-  *row = -1;
-  if (lane < a.T)
-    for (int j = a.topk - 1; j >= 0; --j)
-      if (expert_of(a, a.ids[lane * a.topk + j]) == *e) *row = lane * a.topk + j;
-  return __ballot(*row >= 0) != 0;
+  *tokens = (uint32_t)__ballot(t < a.T && at >= 0);
+  if (*e < 0 || *tokens == 0) return false;
+  // (the first slot that names the expert has it)
+  return !by_slot || __builtin_amdgcn_readlane(at, (int)__builtin_ctz(*tokens)) == u;
 }
 
-template <int D>
-__device__ __forceinline__ float swiglu_sum(const float* lds, int parts, int pitch, int g, int u) {
+// What the second launch needs of a unit, by the unit's first workgroup.
+__device__ __forceinline__ void write_hit(const FewArgs& a, int u, int e, uint32_t tokens) {
+  const int t = threadIdx.x;
+  if (t < MOE_FEW_TOKENS) {
+    float g = 0.f;
+    if ((tokens >> t) & 1)
+      for (int j = 0; j < a.topk; ++j)
+        if (expert_of(a, a.ids[t * a.topk + j]) == e) g += a.gates[t * a.topk + j];
+    a.hits[u].gate[t] = g;
+  }
+  if (t == 0) {
+    a.hits[u].e = e;
+    a.hits[u].tokens = tokens;
+  }
+}
+
+// The unit and tile of a workgroup, and what every first launch does besides; false: nothing
+// to do.
+__device__ __forceinline__ bool begin_up(const FewArgs& a, int* unit, int* tile, int* e, uint32_t* tokens) {
+  *unit = blockIdx.x / a.tiles;
+  *tile = blockIdx.x - *unit * a.tiles;
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i < a.out_tiles; i += blockDim.x) a.count[i] = 0;
+  if (few_unit(a, *unit, e, tokens)) return true;
+  if (*tile == 0) write_hit(a, *unit, -1, 0);
+  return false;
+}
+
+// The lane's sums of column n to LDS [waves][16 tokens][columns].
+template <int COLS>
+__device__ __forceinline__ void put_column(float (*lds)[16][COLS], int n, f32x4 v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) lds[threadIdx.x >> 6][4 * (lane >> 4) + i][n] = v[i];
+}
+
+// silu(gate) * up of the waves' sums, in fp32, rounded once: the second launch's matrix
+// instructions take bf16.
+template <int W, int COLS>
+__device__ __forceinline__ float swiglu(const float (*lds)[16][COLS], int t, int g, int u) {
   float x = 0.f, y = 0.f;
-  for (int p = 0; p < parts; ++p) {
-    x += lds[p * pitch + g];
-    y += lds[p * pitch + u];
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    x += lds[w][t][g];
+    y += lds[w][t][u];
   }
   return x / (1.f + expf(-x)) * y;
 }
 
-template <int C, int D, int W>
+// 64 packed columns (32 outputs), the waves taking every W-th 32 of K.
+constexpr int kCols = 64;
+template <int W>
 __global__ void __launch_bounds__(64 * W) few_up_kernel(FewArgs a) {
-  if (blockIdx.x == gridDim.x - 1) return make_plan(a);
-  constexpr int TOK = 16 / D, COLS = TOK * C;
-  __shared__ float lds[W * D][TOK][COLS];
-  __shared__ int rows[64];
-  int e, tile, row;
-  if (!few_unit(a, &e, &tile, &row)) return;
-  if (threadIdx.x < 64) rows[threadIdx.x] = row;
-  const Lane<D> ln;
-  const int wave = threadIdx.x >> 6, N = 2 * a.I;
-  const int mine = __shfl(row, ln.at);   // of this lane's token
-  const __bf16* x = a.x + (long long)ln.at * a.H;
-  const int col = tile * COLS + ln.at * C;
-  const __bf16* w = (const __bf16*)a.w1 + (long long)e * a.H * N + col;
-  f32x4 acc[C] = {};
-  const int steps = (a.H + 32 * D - 1) / (32 * D);
-  for (int s = wave; s < steps; s += W) {
-    const int k = (s * D + ln.part) * 32 + ln.g * 8;
-    Weights<C> b;
-    b.load(w + (long long)k * N, N, k < a.H && col < N);
-    bf16x8 v = {};
-    if (mine >= 0) v = row8(x, k, a.H);
+  __shared__ float lds[W][16][kCols];
+  int unit, tile, e;
+  uint32_t tokens;
+  if (!begin_up(a, &unit, &tile, &e, &tokens)) return;
+  const int wave = threadIdx.x >> 6, n = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+  const int N = 2 * a.I, col = tile * kCols + 4 * n;
+  const bool mine = (tokens >> n) & 1;
+  const long long bytes = 2LL * a.H * N;
+  const Buffer w = buffer(a.w1 + e * bytes, bytes), x = buffer(a.x, 2LL * a.T * a.H);
+  const uint32_t pitch = 2 * N;
+  f32x4 acc[4] = {};
+  const int steps = (a.H + 31) / 32;
+  run_steps(
+      (steps - wave + W - 1) / W,
+      [&](Bf16Step& b, int i) {
+        const int k = (wave + i * W) * 32 + g * 8;
+        b.load(w, k < a.H && col < N ? k * pitch + 2 * col : kOutOfRange, pitch);
+        b.x = load16(x, k < a.H && mine ? 2u * (n * a.H + k) : kOutOfRange);
+      },
+      [&](const Bf16Step& b, int) {
 #pragma unroll
-    for (int c = 0; c < C; ++c) acc[c] = mfma(v, b.column(c), acc[c]);
-  }
+        for (int c = 0; c < 4; ++c) acc[c] = mfma(b.x, b.column(c), acc[c]);
+      });
 #pragma unroll
-  for (int c = 0; c < C; ++c)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = 4 * ln.g + i;
-      if (r / TOK == ln.part) lds[wave * D + ln.part][r % TOK][ln.at * C + c] = acc[c][i];
-    }
+  for (int c = 0; c < 4; ++c) put_column(lds, 4 * n + c, acc[c]);
   __syncthreads();
-  for (int i = threadIdx.x; i < TOK * COLS / 2; i += 64 * W) {
-    const int t = i / (COLS / 2), c = i % (COLS / 2), at = c / 16 * 32 + c % 16;
-    const float v = swiglu_sum<D>(&lds[0][t][0], W * D, TOK * COLS, at, at + 16);
-    const int r = rows[t];
-    const int o = tile * (COLS / 2) + c;
-    if (r >= 0 && o < a.I) a.act[(long long)r * a.pitch + o] = (__bf16)v;
+  for (int i = threadIdx.x; i < 16 * kCols / 2; i += 64 * W) {
+    const int t = i / (kCols / 2), c = i % (kCols / 2), at = c / 16 * 32 + c % 16, o = tile * (kCols / 2) + c;
+    if (((tokens >> t) & 1) && o < a.I)
+      a.act[((long long)a.T * unit + t) * a.pitch + o] = (__bf16)swiglu<W>(lds, t, at, at + 16);
   }
+  if (tile == 0) write_hit(a, unit, e, tokens);
 }
 
-// Weights in mx4: TOK outputs a workgroup, their gate and their up rows.
-template <int D, int W>
+// 16 G outputs (their gate and their up rows), the waves taking every W-th 16 blocks of K.
+// R: rows of LDS for tokens.
+template <int G, int R, int W, bool kOdd>
 __global__ void __launch_bounds__(64 * W) few_up_mx4_kernel(FewArgs a) {
-  if (blockIdx.x == gridDim.x - 1) return make_plan(a);
-  constexpr int TOK = 16 / D;
-  __shared__ float lds[W * D][TOK][2 * TOK];
-  __shared__ int rows[64];
-  int e, tile, row;
-  if (!few_unit(a, &e, &tile, &row)) return;
-  if (threadIdx.x < 64) rows[threadIdx.x] = row;
-  const Lane<D> ln;
-  const int wave = threadIdx.x >> 6;
-  const int KB = (a.H + kBlock - 1) / kBlock, KS = (KB + 3) / 4 * 4;
-  const int mine = __shfl(row, ln.at);
-  const __bf16* x = a.x + (long long)ln.at * a.H;
-  const int col = tile * TOK + ln.at;
-  const long long rg = (long long)e * 2 * a.I + col, ru = rg + a.I;
-  f32x4 ag = {}, au = {};
-  const int steps = (KB + 4 * D - 1) / (4 * D);
-  for (int s = wave; s < steps; s += W) {
-    const int kb = (s * D + ln.part) * 4 + ln.g;
-    const bool in = kb < KB && col < a.I;
-    Block bg, bu;
-    bg.load(a.w1 + (rg * KB + kb) * 16, a.w1_scales + rg * KS + kb, in);
-    bu.load(a.w1 + (ru * KB + kb) * 16, a.w1_scales + ru * KS + kb, in);
-    bf16x8 v[4] = {};
-    if (mine >= 0) {
+  __shared__ float lds[W][16][32 * G];
+  __shared__ __attribute__((aligned(16))) uint8_t rows[W][R * kStepBytes];
+  int unit, tile, e;
+  uint32_t tokens;
+  if (!begin_up(a, &unit, &tile, &e, &tokens)) return;
+  const int wave = threadIdx.x >> 6, n = threadIdx.x & 15;
+  const int KB = (a.H + kBlock - 1) / kBlock, KS = (KB + 3) / 4 * 4, col = tile * 16 * G + n;
+  const long long codes = 2LL * a.I * KB * 16, scales = 2LL * a.I * KS;
+  const Buffer wc = buffer(a.w1 + e * codes, codes), ws = buffer(a.w1_scales + e * scales, scales);
+  f32x4 acc[2 * G] = {};   // gate and up of the first 16 columns, of the next, ...
+  bool bad[2 * G] = {};
+  const int token = min(n, R - 1);
+  for (int kb0 = wave * kStepBlocks; kb0 < KB; kb0 += W * kStepBlocks) {
+    Mx4Step<2 * G> b;
+    rows_to_lds<kOdd>(rows[wave], a.x, a.T, a.H, tokens, kb0 * kBlock, a.H);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] = row8(x, kb * kBlock + 8 * q, a.H);
+    for (int m = 0; m < 2 * G; ++m) {
+      const int c = col + m / 2 * 16;
+      b.load(m, wc, ws, c + m % 2 * a.I, kb0, KB, KS, c < a.I);
     }
+    waitcnt_vm<0>();
+    asm volatile("" ::: "memory");
+    b.align(kb0, KS);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      ag = mfma(v[q], bg.eight(q), ag);
-      au = mfma(v[q], bu.eight(q), au);
-    }
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const u32x4 v = row_operand(rows[wave], token, j, q);
+#pragma unroll
+        for (int m = 0; m < 2 * G; ++m) acc[m] = mfma(v, b.eight(m, j, q), acc[m]);
+      }
+#pragma unroll
+    for (int m = 0; m < 2 * G; ++m) bad[m] |= b.bad(m, kb0, KB);
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = 4 * ln.g + i;
-    if (r / TOK == ln.part) {
-      lds[wave * D + ln.part][r % TOK][ln.at] = ag[i];
-      lds[wave * D + ln.part][r % TOK][TOK + ln.at] = au[i];
-    }
-  }
+  for (int m = 0; m < 2 * G; ++m) put_column(lds, 16 * m + n, with_nan(acc[m], bad[m]));
   __syncthreads();
-  for (int i = threadIdx.x; i < TOK * TOK; i += 64 * W) {
-    const int t = i / TOK, c = i % TOK;
-    const float v = swiglu_sum<D>(&lds[0][t][0], W * D, 2 * TOK * TOK, c, TOK + c);
-    const int r = rows[t];
-    const int o = tile * TOK + c;
-    if (r >= 0 && o < a.pitch) a.act[(long long)r * a.pitch + o] = (__bf16)(o < a.I ? v : 0.f);
+  for (int i = threadIdx.x; i < 256 * G; i += 64 * W) {
+    const int t = i / (16 * G), c = i % (16 * G), o = tile * 16 * G + c, at = c / 16 * 32 + c % 16;
+    if (((tokens >> t) & 1) && o < a.pitch)
+      a.act[((long long)a.T * unit + t) * a.pitch + o] = (__bf16)(o < a.I ? swiglu<W>(lds, t, at, at + 16) : 0.f);
   }
+  if (tile == 0) write_hit(a, unit, e, tokens);
 }
 
 // ---- the second launch -------------------------------------------------------------------
 //
-// A workgroup takes a tile of out's columns through every hit expert; its waves share the
-// experts' K.  A wave adds an expert's part to its sums, weighted and only for the tokens
-// that name it, before it goes on to the next; the waves' sums are joined in LDS, in order.
-template <int C, int D, int W, bool kMx4>
-__global__ void __launch_bounds__(64 * W) few_down_kernel(FewArgs a) {
-  constexpr int TOK = 16 / D, COLS = TOK * C;
-  __shared__ float lds[W * D][TOK][COLS];
-  const Lane<D> ln;
-  const int wave = threadIdx.x >> 6;
-  const int col = blockIdx.x * COLS + ln.at * C;
-  const int KB = (a.I + kBlock - 1) / kBlock, KS = (KB + 3) / 4 * 4;
-  const int steps = kMx4 ? (KB + 4 * D - 1) / (4 * D) : (a.I + 32 * D - 1) / (32 * D);
-  const int n = a.plan->n;
-  const int s0 = (int)((long long)n * steps * wave / W), s1 = (int)((long long)n * steps * (wave + 1) / W);
-  f32x4 acc[C] = {}, sum[C] = {};
-  int u = s0 / steps, s = s0 - u * steps;
-  for (int at = s0; at < s1; ++at) {
-    const Hit* h = &a.plan->hit[u];
-    const int e = h->e, row = h->row[ln.at];
-    const __bf16* x = a.act + (long long)row * a.pitch;
-    if constexpr (kMx4) {
-      const int kb = (s * D + ln.part) * 4 + ln.g;
-      const long long r = (long long)e * a.H + col;
-      Block b;
-      b.load(a.w2 + (r * KB + kb) * 16, a.w2_scales + r * KS + kb, kb < KB && col < a.H);
-      bf16x8 v[4] = {};
-      if (row >= 0 && kb < KB) {
+// A workgroup takes a tile of out's columns through a share of the hit experts' K; the
+// waves of a tile's workgroups share it evenly.  A wave adds an expert's part to its sums,
+// weighted and only for the tokens that name it, before it goes on to the next; the waves'
+// sums are joined in LDS, and the shares' by the last of a tile's workgroups to end, both
+// in a fixed order.
+
+// The hit experts, in the order of their units, to `hits`: the expert, and its tokens with
+// the unit in the high half.  Returns how many.
+template <int W>
+__device__ __forceinline__ int list_hits(const FewArgs& a, int2* hits) {
+  __shared__ int ends[W];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int n = 0;
+  for (int u0 = 0; u0 < a.units; u0 += 64 * W) {
+    const int u = u0 + threadIdx.x;
+    int2 h = {-1, 0};
+    if (u < a.units) h = *(const int2*)&a.hits[u];
+    const uint64_t m = __ballot(h.x >= 0);
+    if (lane == 0) ends[wave] = __popcll(m);
+    __syncthreads();
+    int before = n;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = row8(x, kb * kBlock + 8 * q, a.pitch);
-      }
-#pragma unroll
-      for (int q = 0; q < 4; ++q) acc[0] = mfma(v[q], b.eight(q), acc[0]);
-    } else {
-      const int k = (s * D + ln.part) * 32 + ln.g * 8;
-      Weights<C> b;
-      b.load((const __bf16*)a.w2 + ((long long)e * a.I + k) * a.H + col, a.H, k < a.I && col < a.H);
-      bf16x8 v = {};
-      if (row >= 0) v = row8(x, k, a.I);
-#pragma unroll
-      for (int c = 0; c < C; ++c) acc[c] = mfma(v, b.column(c), acc[c]);
+    for (int w = 0; w < W; ++w) {
+      before += w < wave ? ends[w] : 0;
+      n += ends[w];
     }
-    if (++s == steps || at + 1 == s1) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int t = (4 * ln.g + i) % TOK;
-        const bool on = h->row[t] >= 0;
-        const float g = h->gate[t];
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          sum[c][i] = on ? fmaf(g, acc[c][i], sum[c][i]) : sum[c][i];
-          acc[c][i] = 0.f;
-        }
-      }
-      s = 0;
-      ++u;
-    }
+    if (h.x >= 0) hits[before + __popcll(m & ((1ull << lane) - 1))] = {h.x, h.y | u << 16};
+    __syncthreads();
   }
+  return n;
+}
+
+// A wave's steps s0 .. s1 of the n experts' `steps` each, and where they begin.
+struct Part {
+  int s0, s1, u, s;
+  template <int W>
+  static __device__ __forceinline__ Part of(int n, int steps, int share, int shares, int wave) {
+    const int all = shares * W, mine = share * W + wave, total = n * steps, each = total / all, more = total - each * all;
+    Part p;
+    p.s0 = mine * each + min(mine, more);
+    p.s1 = p.s0 + each + (mine < more);
+    p.u = p.s0 / steps;
+    p.s = p.s0 - p.u * steps;
+    return p;
+  }
+};
+
+// The gates and tokens of a hit, for the four rows of the lane's results.
+struct Gates {
+  f32x4 gate;
+  uint32_t tokens;
+  __device__ __forceinline__ void load(const FewArgs& a, int2 hit) {
+    tokens = (uint32_t)hit.y >> (4 * ((threadIdx.x & 63) >> 4));
+    const float* p = a.hits[(uint32_t)hit.y >> 16].gate + 4 * ((threadIdx.x & 63) >> 4);
 #pragma unroll
-  for (int c = 0; c < C; ++c)
+    for (int i = 0; i < 4; ++i) gate[i] = p[i];
+  }
+  __device__ __forceinline__ void add(f32x4& sum, f32x4& acc) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int r = 4 * ln.g + i;
-      if (r / TOK == ln.part) lds[wave * D + ln.part][r % TOK][ln.at * C + c] = sum[c][i];
-    }
-  __syncthreads();
-  for (int i = threadIdx.x; i < TOK * COLS; i += 64 * W) {
-    const int t = i / COLS, c = i % COLS, o = blockIdx.x * COLS + c;
-    float v = 0.f;
-    for (int p = 0; p < W * D; ++p) v += lds[p][t][c];
-    if (t < a.T && o < a.H) {
-      if (a.out16)
-        ((__bf16*)a.out)[(long long)t * a.H + o] = (__bf16)v;
-      else
-        ((float*)a.out)[(long long)t * a.H + o] = v;
+      sum[i] = (tokens >> i) & 1 ? fmaf(gate[i], acc[i], sum[i]) : sum[i];
+      acc[i] = 0.f;
     }
   }
+};
+
+__device__ __forceinline__ void put_out(const FewArgs& a, int t, int o, float v) {
+  if (a.out16)
+    ((__bf16*)a.out)[(long long)t * a.H + o] = (__bf16)v;
+  else
+    ((float*)a.out)[(long long)t * a.H + o] = v;
+}
+
+// The waves' sums of COLS columns from LDS, and the shares', to out.
+template <int W, int COLS>
+__device__ __forceinline__ void join_sums(const FewArgs& a, const float (*lds)[16][COLS], int share, int tile) {
+  __shared__ bool last;
+  __syncthreads();
+  for (int i = threadIdx.x; i < a.T * COLS; i += 64 * W) {
+    const int t = i / COLS, c = i % COLS, o = tile * COLS + c;
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) v += lds[w][t][c];
+    if (o < a.H) {
+      if (a.shares == 1)
+        put_out(a, t, o, v);
+      else
+        __hip_atomic_store(a.parts + ((long long)share * a.T + t) * a.H + o, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+  }
+  if (a.shares == 1) return;
+  // A share's sums have left for good before it counts itself: they are stored past the L2
+  // (as agent-scope atomics), so that each wave waits for its own stores and no cache is
+  // written back (a release fence by every wave took 25 us).
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0)
+    last = __hip_atomic_fetch_add(a.count + tile, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)a.shares - 1;
+  __syncthreads();
+  if (!last) return;
+  for (int i = threadIdx.x; i < a.T * COLS; i += 64 * W) {
+    const int t = i / COLS, c = i % COLS, o = tile * COLS + c;
+    if (o >= a.H) continue;
+    float part[kMaxShares], v = 0.f;   // (all of them on their way together)
+#pragma unroll
+    for (int p = 0; p < kMaxShares; ++p)
+      if (p < a.shares)
+        part[p] = __hip_atomic_load(a.parts + ((long long)p * a.T + t) * a.H + o, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+    for (int p = 0; p < kMaxShares; ++p)
+      if (p < a.shares) v += part[p];
+    put_out(a, t, o, v);
+  }
+}
+
+template <int W>
+__global__ void __launch_bounds__(64 * W) few_down_kernel(FewArgs a) {
+  __shared__ float lds[W][16][kCols];
+  __shared__ int2 hits[kMaxExperts];
+  const int share = blockIdx.x / a.out_tiles, tile = blockIdx.x - share * a.out_tiles;
+  const int wave = threadIdx.x >> 6, n = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+  const int col = tile * kCols + 4 * n, steps = (a.I + 31) / 32;
+  const Part p = Part::of<W>(list_hits<W>(a, hits), steps, share, a.shares, wave);
+  f32x4 acc[4] = {}, sum[4] = {};
+  Gates gates;
+  int load_u = p.u, load_s = p.s, u = p.u, s = p.s;   // the places of the next load and the next products
+  if (p.s0 < p.s1) {
+    gates.load(a, hits[u]);
+    run_steps(
+        p.s1 - p.s0,
+        [&](Bf16Step& b, int i) {
+          const bool live = p.s0 + i < p.s1;
+          const int2 h = hits[live ? load_u : p.u];
+          const int e = __builtin_amdgcn_readfirstlane(h.x);
+          const uint32_t tokens = __builtin_amdgcn_readfirstlane(h.y);
+          const long long bytes = 2LL * a.I * a.H;
+          const int k = load_s * 32 + g * 8;
+          const bool in = live && k < a.I;
+          b.load(buffer(a.w2 + e * bytes, bytes), in && col < a.H ? (uint32_t)(k * a.H + col) * 2 : kOutOfRange, 2 * a.H);
+          b.x = load16(buffer(a.act + (long long)a.T * (tokens >> 16) * a.pitch, 2LL * a.T * a.pitch),
+                       in && ((tokens >> n) & 1) ? 2u * (n * a.pitch + k) : kOutOfRange);
+          if (++load_s == steps) load_s = 0, ++load_u;
+        },
+        [&](const Bf16Step& b, int i) {
+          const int at = p.s0 + i;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) acc[c] = mfma(b.x, b.column(c), acc[c]);
+          if (at < p.s1 && (s + 1 == steps || at + 1 == p.s1)) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) gates.add(sum[c], acc[c]);
+            if (at + 1 < p.s1) gates.load(a, hits[u + 1]);
+          }
+          if (++s == steps) s = 0, ++u;
+        });
+  }
+#pragma unroll
+  for (int c = 0; c < 4; ++c) put_column(lds, 4 * n + c, sum[c]);
+  join_sums<W>(a, lds, share, tile);
+}
+
+// Weights in mx4: 16 columns, a wave's step as in the first launch.
+template <int R, int W>
+__global__ void __launch_bounds__(64 * W) few_down_mx4_kernel(FewArgs a) {
+  __shared__ float lds[W][16][16];
+  __shared__ int2 hits[kMaxExperts];
+  __shared__ __attribute__((aligned(16))) uint8_t rows[W][R * kStepBytes];
+  const int share = blockIdx.x / a.out_tiles, tile = blockIdx.x - share * a.out_tiles;
+  const int wave = threadIdx.x >> 6, n = threadIdx.x & 15;
+  const int KB = a.pitch / kBlock, KS = (KB + 3) / 4 * 4, col = tile * 16 + n;
+  const int steps = (KB + kStepBlocks - 1) / kStepBlocks;
+  const long long codes = 16LL * a.H * KB, scales = (long long)a.H * KS;
+  const Part p = Part::of<W>(list_hits<W>(a, hits), steps, share, a.shares, wave);
+  f32x4 acc = {}, sum = {};
+  bool bad = false;
+  int u = p.u, s = p.s;
+  for (int at = p.s0; at < p.s1; ++at) {
+    const int2 h = hits[u];
+    const int e = __builtin_amdgcn_readfirstlane(h.x), kb0 = s * kStepBlocks;
+    const uint32_t tokens = __builtin_amdgcn_readfirstlane(h.y);
+    Mx4Step<1> b;
+    Gates gates;
+    const bool ends = s + 1 == steps || at + 1 == p.s1;
+    rows_to_lds<false>(rows[wave], a.act + (long long)a.T * (tokens >> 16) * a.pitch, a.T, a.pitch, tokens & 0xffff,
+                       kb0 * kBlock, a.pitch);
+    b.load(0, buffer(a.w2 + e * codes, codes), buffer(a.w2_scales + e * scales, scales), col, kb0, KB, KS, col < a.H);
+    if (ends) gates.load(a, h);
+    waitcnt_vm<0>();
+    asm volatile("" ::: "memory");
+    b.align(kb0, KS);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) acc = mfma(row_operand(rows[wave], min(n, R - 1), j, q), b.eight(0, j, q), acc);
+    bad |= b.bad(0, kb0, KB);
+    if (ends) {
+      acc = with_nan(acc, bad);
+      gates.add(sum, acc);
+      bad = false;
+    }
+    if (++s == steps) s = 0, ++u;
+  }
+  put_column(lds, n, sum);
+  join_sums<W>(a, lds, share, tile);
 }
 
 // ---- host ----------------------------------------------------------------------------------
 
-size_t plan_bytes(int slots) {
-  return sizeof(Plan) - sizeof(Hit) + sizeof(Hit) * (size_t)(slots < kMaxExperts ? slots : kMaxExperts);
-}
 int act_pitch(int I) { return (I + kBlock - 1) / kBlock * kBlock; }
+size_t up16(size_t n) { return (n + 15) / 16 * 16; }
+
+// The second launch: columns of a tile, waves of a workgroup, and the shares of a tile's
+// work: as many as there are CUs for, while every wave keeps a step.  (us, 32 experts, top 6,
+// 2048 x 704: bf16, one token 12.6, 6.6, 6.5 with 1, 4, 8 shares, 16 tokens 77, 24, 18; mx4, 16
+// tokens 14.3, 10.4, 13.0 with 1, 2, 4, and 5 tokens of 11 experts of 1352 x 336 4.6 and 6.3
+// with 1 and 2, half of the waves without a step.)
+struct Down {
+  int cols, waves, tiles, shares;
+};
+Down down_of(bool mx4, int T, int H, int I, int units) {
+  Down d;
+  d.cols = mx4 ? 16 : kCols;
+  d.waves = mx4 && T <= 4 ? 16 : 8;
+  d.tiles = (H + d.cols - 1) / d.cols;
+  const int k = mx4 ? kStepK : 32;
+  const long long steps = (long long)units * ((I + k - 1) / k);
+  d.shares = 1;
+  while (d.shares < kMaxShares && 2 * d.shares * d.tiles <= 256 && steps >= 2 * d.shares * d.waves) d.shares *= 2;
+  return d;
+}
+
+// Scratch: the units, the activations, the shares' counts and their sums.
+struct Layout {
+  size_t act, count, parts, bytes;
+};
+Layout layout_of(int T, int H, int I, int E, int topk) {
+  const size_t units = T * topk < E ? T * topk : E;
+  Layout l;
+  l.act = up16(units * sizeof(Hit));
+  l.count = l.act + up16(units * T * act_pitch(I) * sizeof(__bf16));
+  l.parts = l.count + up16((size_t)(H + 15) / 16 * sizeof(uint32_t));
+  size_t parts = 0;
+  for (const bool mx4 : {false, true}) {
+    const Down d = down_of(mx4, T, H, I, (int)units);
+    const size_t n = d.shares > 1 ? (size_t)d.shares * T * H * sizeof(float) : 0;
+    parts = n > parts ? n : parts;
+  }
+  l.bytes = l.parts + up16(parts);
+  return l;
+}
 
 int few(bool mx4, const void* hidden, const void* w1, const void* w1_scales, const void* w2, const void* w2_scales,
         const int32_t* ids, const float* gates, void* out, int32_t T, int32_t H, int32_t I, int32_t E, int32_t topk,
@@ -438,8 +636,9 @@ int few(bool mx4, const void* hidden, const void* w1, const void* w1_scales, con
   if ((long long)units * (act_pitch(I) / 16) > (1 << 22)) return MOE_ERR_UNSUPPORTED;
   if (T == 0) return MOE_OK;
   if (!hidden || !w1 || !w2 || !ids || !gates || !out || (mx4 && (!w1_scales || !w2_scales))) return MOE_ERR_INVALID_ARG;
-  if (!scratch || scratch_bytes < moe_few_scratch_size(T, I, topk)) return MOE_ERR_WORKSPACE;
-  if (!aligned(hidden, 2) || !aligned(w1, 16) || !aligned(w2, 16) || !aligned(ids, 4) || !aligned(gates, 4) ||
+  const Layout l = layout_of(T, H, I, E, topk);
+  if (!scratch || scratch_bytes < l.bytes) return MOE_ERR_WORKSPACE;
+  if (!aligned(hidden, 16) || !aligned(w1, 16) || !aligned(w2, 16) || !aligned(ids, 4) || !aligned(gates, 4) ||
       !aligned(out, type_size(out_type)) || !aligned(scratch, 16))
     return MOE_ERR_ALIGNMENT;
   if (mx4 && (!aligned(w1_scales, 4) || !aligned(w2_scales, 4))) return MOE_ERR_ALIGNMENT;
@@ -450,30 +649,47 @@ int few(bool mx4, const void* hidden, const void* w1, const void* w1_scales, con
   a.w1 = (const uint8_t*)w1, a.w1_scales = (const uint8_t*)w1_scales;
   a.w2 = (const uint8_t*)w2, a.w2_scales = (const uint8_t*)w2_scales;
   a.ids = ids, a.gates = gates, a.out = out;
-  a.plan = (Plan*)scratch;
-  a.act = (__bf16*)((char*)scratch + plan_bytes(T * topk));
+  a.hits = (Hit*)scratch;
+  a.act = (__bf16*)((char*)scratch + l.act);
+  a.count = (uint32_t*)((char*)scratch + l.count);
+  a.parts = (float*)((char*)scratch + l.parts);
   a.T = T, a.H = H, a.I = I, a.E = E, a.topk = topk, a.first = first;
-  a.slots = T * topk, a.pitch = act_pitch(I), a.out16 = out_type == MOE_BF16;
+  a.slots = T * topk, a.units = units, a.pitch = act_pitch(I), a.out16 = out_type == MOE_BF16;
+  const Down d = down_of(mx4, T, H, I, units);
+  a.out_tiles = d.tiles, a.shares = d.shares;
   const hipStream_t s = (hipStream_t)stream;
-  if (mx4) {
-    a.tiles = (a.pitch + 15) / 16;
-    few_up_mx4_kernel<1, 8><<<(unsigned)(units * a.tiles + 1), 512, 0, s>>>(a);
-    if (hipGetLastError() != hipSuccess) return MOE_ERR_HIP;
-    few_down_kernel<1, 1, 16, true><<<(unsigned)((H + 15) / 16), 1024, 0, s>>>(a);
+  // Variants by the rows that tokens take in LDS (which bounds how many waves a CU holds), and
+  // beyond eight tokens two waves a workgroup, with two tiles where K is long (16 tokens: H =
+  // 2048 17.9 us with one tile and 15.6 with two, H = 1024 8.8 and 10.3).
+  const bool odd = H % kBlock != 0;
+  if (!mx4) {
+    a.tiles = (2 * I + kCols - 1) / kCols;
+    few_up_kernel<8><<<(unsigned)(units * a.tiles), 64 * 8, 0, s>>>(a);
   } else {
-    a.tiles = (2 * I + 31) / 32;
-    few_up_kernel<2, 1, 8><<<(unsigned)(units * a.tiles + 1), 512, 0, s>>>(a);
-    if (hipGetLastError() != hipSuccess) return MOE_ERR_HIP;
-    few_down_kernel<2, 1, 16, false><<<(unsigned)((H + 31) / 32), 1024, 0, s>>>(a);
+    const int groups = T > 8 && H > 1024 ? 2 : 1, waves = T > 8 ? 2 : 4;
+    a.tiles = (a.pitch + 16 * groups - 1) / (16 * groups);
+    auto up = T <= 4      ? (odd ? few_up_mx4_kernel<1, 4, 4, true> : few_up_mx4_kernel<1, 4, 4, false>)
+              : T <= 8    ? (odd ? few_up_mx4_kernel<1, 8, 4, true> : few_up_mx4_kernel<1, 8, 4, false>)
+              : groups > 1 ? (odd ? few_up_mx4_kernel<2, 16, 2, true> : few_up_mx4_kernel<2, 16, 2, false>)
+                           : (odd ? few_up_mx4_kernel<1, 16, 2, true> : few_up_mx4_kernel<1, 16, 2, false>);
+    up<<<(unsigned)(units * a.tiles), 64 * waves, 0, s>>>(a);
   }
+  if (hipGetLastError() != hipSuccess) return MOE_ERR_HIP;
+  auto down = !mx4     ? few_down_kernel<8>
+              : T <= 4 ? few_down_mx4_kernel<4, 16>
+              : T <= 8 ? few_down_mx4_kernel<8, 8>
+                       : few_down_mx4_kernel<16, 8>;
+  down<<<(unsigned)(d.tiles * d.shares), 64 * d.waves, 0, s>>>(a);
   return done();
 }
 
 }  // namespace
 
-extern "C" size_t moe_few_scratch_size(int32_t T, int32_t I, int32_t topk) {
-  if (T < 1 || T > MOE_FEW_TOKENS || I < 1 || I > kMaxWidth || topk < 1 || topk > kMaxTopk) return 0;
-  return plan_bytes(T * topk) + (size_t)T * topk * act_pitch(I) * sizeof(__bf16);
+extern "C" size_t moe_few_scratch_size(int32_t T, int32_t H, int32_t I, int32_t E, int32_t topk) {
+  if (T < 1 || T > MOE_FEW_TOKENS || H < 1 || H > kMaxWidth || I < 1 || I > kMaxWidth || E < 1 || E > kMaxExperts ||
+      topk < 1 || topk > kMaxTopk)
+    return 0;
+  return layout_of(T, H, I, E, topk).bytes;
 }
 
 extern "C" int moe_few_forward(const void* hidden, const void* w1, const void* w2, const int32_t* ids,

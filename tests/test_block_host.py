@@ -124,10 +124,11 @@ def test_few_refusals(mx4):
         assert _few(mx4, s1=P + 2) == _few(mx4, s2=P + 1) == B.MOE_ERR_ALIGNMENT
     else:
         assert _few(mx4, H=60) == _few(mx4, I=24) == B.MOE_ERR_UNSUPPORTED
-    need = K.layer_few_scratch_size(2, 32, 2)
+    need = K.layer_few_scratch_size(2, 64, 32, 4, 2)
     assert need >= 2 * 4 * 32
     assert _few(mx4, scratch=None) == _few(mx4, room=need - 1) == B.MOE_ERR_WORKSPACE
-    assert K.layer_few_scratch_size(17, 32, 2) == K.layer_few_scratch_size(2, 0, 2) == K.layer_few_scratch_size(2, 2, 65) == 0
+    for bad in ((17, 64, 32, 4, 2), (2, 64, 0, 4, 2), (2, 64, 32, 4, 65), (2, 0, 32, 4, 2), (2, 64, 32, 1025, 2), (2 ** 40, 8, 8, 8, 8)):
+        assert K.layer_few_scratch_size(*bad) == 0
     assert _few(mx4, T=0, x=None, ids=None, gates=None, out=None, scratch=None, room=0) == B.MOE_OK
 
 

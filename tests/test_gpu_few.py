@@ -39,15 +39,16 @@ def _case(T, H, I, E, k, drop=0.0, seed=0, repeat=False):
     return ids, gates, x, w1, w2
 
 
-def _run(case, weights, dtype="float32", first=0, poison=True):
+def _run(case, weights, dtype="float32", first=0):
     """layer_few into an output of NaN, with scratch of NaN bytes and no byte to spare."""
     import torch
     K = _K()
     ids, gates, x = case[:3]
     T, H = x.shape
-    I = weights[1].K if isinstance(weights[1], tuple) else weights[1].shape[1]
+    mx4 = isinstance(weights[1], tuple)
+    I, E = (weights[1].K, weights[1].codes.shape[0]) if mx4 else (weights[1].shape[1], weights[1].shape[0])
     out = torch.full((T, H), float("nan"), dtype=getattr(torch, dtype), device="cuda")
-    n = K.layer_few_scratch_size(T, I, ids.shape[1])
+    n = K.layer_few_scratch_size(T, H, I, E, ids.shape[1])
     base = torch.full((n + 256,), 255, dtype=torch.uint8, device="cuda")
     got = K.layer_few(x.cuda(), *weights, torch.from_numpy(ids).cuda(), torch.from_numpy(gates).cuda(),
                       first_expert=first, out=out, scratch=base[:n])
