@@ -76,81 +76,95 @@ __device__ __forceinline__ void load_logits(const T* p, int E, int l, float (&v)
 
 __device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
 
+// A float's bits in an order that integers compare by (NaN aside), and back.
+__device__ __forceinline__ int ordered(float v) {
+  const int b = __float_as_int(v);
+  return b ^ ((b >> 31) & 0x7fffffff);
+}
+__device__ __forceinline__ float unordered(int k) { return __int_as_float(k ^ ((k >> 31) & 0x7fffffff)); }
+
+// Bound by the instructions of the rounds (two comparisons and two selections for each
+// logit of a lane): 16384 tokens, 8 of 256 experts, by sixteen lanes a token.  The scores are
+// taken of the chosen alone, spread over the lanes: slot j is lane j % L's.
 template <class T, int L, int R>
 __global__ void __launch_bounds__(256) choose_kernel(const T* logits, const float* bias, int32_t* ids, float* gates,
-                                                     long long first, int tokens, int E, int topk, bool softmax, bool renorm,
-                                                     float scale) {
+                                                     long long first, int tokens, int E, int topk, bool softmax,
+                                                     bool renorm, float scale) {
+  constexpr int S = L == 64 ? 1 : 4;   // slots of a lane
   const int l = threadIdx.x % L;
   const long long t0 = first + (long long)blockIdx.x * (256 / L) + threadIdx.x / L;
   const bool in = t0 < tokens;
   const long long t = in ? t0 : tokens - 1;   // (groups past the last token do its work again, and write nothing)
-  float v[R], key[R], b[R];
+  float v[R], b[R];
   load_logits<T, L, R>(logits + t * E, E, l, v);
   if (bias) load_logits<float, L, R>(bias, E, l, b);
-  int slot[R];
-  float top = kNone;
+  const int none = ordered(kNone);
+  int key[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const int e = 4 * (r / 4 * L + l) + r % 4;
-    top = fmaxf(top, v[r]);
-    key[r] = bias ? v[r] + b[r] : v[r] + 0.f;   // (+ 0: equal to every comparison, -0 among them)
-    if (!(key[r] > kNone) || e >= E) key[r] = kNone;
-    slot[r] = -1;
+    const float k = bias ? v[r] + b[r] : v[r] + 0.f;   // (+ 0: -0 and 0 are equal)
+    key[r] = k > kNone ? ordered(k + 0.f) : none;      // (past E: kNone)
   }
-  int n = 0;
-  for (; n < topk; ++n) {
-    float best = key[0];
+  int id[S];
+  float chosen[S];
 #pragma unroll
-    for (int r = 1; r < R; ++r) best = fmaxf(best, key[r]);
-    best = max_of<L>(best);
-    if (__ballot(best > kNone) == 0) break;   // no token of the wave has another
+  for (int s = 0; s < S; ++s) id[s] = -1, chosen[s] = kNone;
+  for (int n = 0; n < topk; ++n) {
+    int best = key[0];
+#pragma unroll
+    for (int r = 1; r < R; ++r) best = max(best, key[r]);
+    best = over_lanes<L>(best, [](int x, int y) { return max(x, y); });
+    if (__ballot(best > none) == 0) break;   // no token of the wave has another
     int e = INT32_MAX;
 #pragma unroll
-    for (int r = R - 1; r >= 0; --r)
-      if (key[r] == best) e = 4 * (r / 4 * L + l) + r % 4;
-    e = min_of<L>(best > kNone ? e : INT32_MAX);
+    for (int r = R - 1; r >= 0; --r) e = key[r] == best ? 4 * (r / 4 * L + l) + r % 4 : e;
+    e = min_of<L>(best > none ? e : INT32_MAX);
+    float x = kNone;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const bool it = e == 4 * (r / 4 * L + l) + r % 4;
+      key[r] = it ? none : key[r];
+      if (bias) x = it ? v[r] : x;
+    }
+    x = bias ? max_of<L>(x) : unordered(best);
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+      if (n == s * L + l && best > none) id[s] = e, chosen[s] = x;
+  }
+  const bool all = softmax && !renorm;
+  float shift = kNone, sum = 0.f, p[S];
+  if (all) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) shift = fmaxf(shift, v[r]);
+  } else {
+#pragma unroll
+    for (int s = 0; s < S; ++s) shift = fmaxf(shift, softmax ? chosen[s] : fminf(chosen[s], 0.f));
+  }
+  shift = max_of<L>(shift);
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+    p[s] = 0.f;
+    if (id[s] < 0) continue;
+    // (renormalised sigmoids by their ratio to the largest: none is lost to underflow)
+    p[s] = softmax ? expf(chosen[s] - shift)
+           : renorm ? expf(fminf(chosen[s], 0.f) - shift) / (1.f + expf(-fabsf(chosen[s])))
+                    : sigmoid(chosen[s]);
+    if (renorm) sum += p[s];
+  }
+  if (all) {
 #pragma unroll
     for (int r = 0; r < R; ++r)
-      if (e == 4 * (r / 4 * L + l) + r % 4) {
-        slot[r] = n;
-        key[r] = kNone;
-      }
-  }
-  // p of the chosen, and what they are divided by
-  float shift = kNone, sum = 0.f, p[R];
-#pragma unroll
-  for (int r = 0; r < R; ++r)
-    if (slot[r] >= 0) shift = fmaxf(shift, softmax || !renorm ? v[r] : fminf(v[r], 0.f));
-  shift = max_of<L>(softmax && !renorm ? top : shift);
-  int chosen = 0;
-#pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const bool on = slot[r] >= 0, all = softmax && !renorm;
-    p[r] = 0.f;
-    if (on || all) {
-      // (renormalised sigmoids by their ratio to the largest: none is lost to underflow)
-      p[r] = softmax ? expf(v[r] - shift)
-             : renorm ? expf(fminf(v[r], 0.f) - shift) / (1.f + expf(-fabsf(v[r])))
-                      : sigmoid(v[r]);
-      const int e = 4 * (r / 4 * L + l) + r % 4;
-      if (all ? e < E : on) sum += p[r];
-    }
-    chosen += on;
+      if (4 * (r / 4 * L + l) + r % 4 < E) sum += expf(v[r] - shift);
   }
   sum = sum_of<L>(sum);
   const float f = softmax || renorm ? scale / sum : scale;
-  const int used = over_lanes<L>(chosen, [](int a, int b) { return a + b; });
   if (!in) return;
 #pragma unroll
-  for (int r = 0; r < R; ++r)
-    if (slot[r] >= 0) {
-      ids[t * topk + slot[r]] = 4 * (r / 4 * L + l) + r % 4;
-      gates[t * topk + slot[r]] = p[r] * f;
+  for (int s = 0; s < S; ++s)
+    if (s * L + l < topk) {
+      ids[t * topk + s * L + l] = id[s];
+      gates[t * topk + s * L + l] = id[s] < 0 ? 0.f : p[s] * f;
     }
-  for (int j = used + l; j < topk; j += L) {
-    ids[t * topk + j] = -1;
-    gates[t * topk + j] = 0.f;
-  }
 }
 
 // With q_j the gates over `scale`, the chosen slots' gradients g_j, and G = sum q_j g_j:
@@ -247,6 +261,7 @@ __global__ void __launch_bounds__(256) choose_grad_kernel(const float* dgates, c
 
 // Eight elements of a row as they lie in memory, bf16 in `a` alone: loaded together
 // whatever their types are, and converted where they are used.
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4_2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x4_4 __attribute__((ext_vector_type(4), aligned(4)));
@@ -263,20 +278,24 @@ __device__ __forceinline__ Raw load8(const void* p, bool bf16, long long at, int
       r.a = *(const u32x4_4*)((const uint32_t*)p + at);
       r.b = *(const u32x4_4*)((const uint32_t*)p + at + 4);
     }
-  } else if (n > 0) {
+  } else if (n > 0) {   // (the last one again instead of those past the end: no load waits for a test)
     if (bf16) {
       const uint16_t* q = (const uint16_t*)p + at;
+      uint32_t v[7];
 #pragma unroll
-      for (int i = 0; i < 7; ++i)
-        if (i < n) r.a[i / 2] |= (uint32_t)q[i] << (16 * (i % 2));
+      for (int i = 0; i < 7; ++i) v[i] = q[min(i, n - 1)];
+#pragma unroll
+      for (int i = 0; i < 7; ++i) r.a[i / 2] |= i < n ? v[i] << (16 * (i % 2)) : 0;
     } else {
       const uint32_t* q = (const uint32_t*)p + at;
+      uint32_t v[7];
 #pragma unroll
-      for (int i = 0; i < 7; ++i)
-        if (i < n) {
-          if (i < 4) r.a[i % 4] = q[i];
-          else r.b[i % 4] = q[i];
-        }
+      for (int i = 0; i < 7; ++i) v[i] = q[min(i, n - 1)];
+#pragma unroll
+      for (int i = 0; i < 7; ++i) {
+        if (i < 4) r.a[i % 4] = i < n ? v[i] : 0;
+        else r.b[i % 4] = i < n ? v[i] : 0;
+      }
     }
   }
   return r;
@@ -480,148 +499,257 @@ __global__ void __launch_bounds__(NT) join_kernel(JoinArgs a, long long first) {
 // The gradient: with v = dz before, r the norm's factor and D = dx + r (v - x r^2
 // mean(x v)), dh = D, da = scale drop(D), db = gate da, and dy is db or, by the same
 // formula, its way back through the norm after the block.  Workgroup g takes rows g,
-// g + G, ...; its sums over rows of the columns' gradients stay in registers, go to
-// `parts` [array][G][H] and are added up by a second launch, always in the same order.
-// Bound by memory.
-template <int NT, int U>
+// g + G, ..., the next one's loads under way while it works on one, four columns a thread (so
+// that what a thread keeps fits its registers); its sums over rows of the columns'
+// gradients go to `parts` [array][G][H] and are added up by a second launch, always in the
+// same order.  Rows of up to 4096 columns keep these sums, and the weights, in registers;
+// longer ones (kLong) keep the sums in LDS and load weights and columns again.  Bound by memory.
+// Types are the kernel's own (B16: bf16, else fp32), so that a row is as few registers as it
+// is bytes; kY: with a norm after the block or a gate (else y is not read).
+template <bool B16>
+struct Four;
+template <>
+struct Four<true> {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  typedef uint32_t u32x2_2 __attribute__((ext_vector_type(2), aligned(2)));
+  u32x2 a;
+  __device__ __forceinline__ void load(const void* p, long long at, int n) {
+    const uint16_t* q = (const uint16_t*)p + at;
+    a = u32x2{0, 0};
+    if (n >= 4) {
+      a = *(const u32x2_2*)q;
+    } else if (n > 0) {
+      const uint32_t v[3] = {q[0], q[min(1, n - 1)], q[min(2, n - 1)]};
+      a = u32x2{v[0] | (n > 1 ? v[1] << 16 : 0), n > 2 ? v[2] : 0};
+    }
+  }
+  __device__ __forceinline__ f32x4 get() const {
+    return {__uint_as_float(a[0] << 16), __uint_as_float(a[0] & 0xffff0000u), __uint_as_float(a[1] << 16),
+            __uint_as_float(a[1] & 0xffff0000u)};
+  }
+  static __device__ __forceinline__ void put(void* p, long long at, int n, f32x4 v) {
+    __bf16* q = (__bf16*)p + at;
+    typedef __bf16 b16x4 __attribute__((ext_vector_type(4)));
+    typedef __bf16 b16x4_2 __attribute__((ext_vector_type(4), aligned(2)));
+    if (n >= 4) {
+      *(b16x4_2*)q = b16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+    } else {
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+        if (i < n) q[i] = (__bf16)v[i];
+    }
+  }
+};
+template <>
+struct Four<false> {
+  typedef float f32x4_4 __attribute__((ext_vector_type(4), aligned(4)));
+  f32x4 a;
+  __device__ __forceinline__ void load(const void* p, long long at, int n) {
+    const float* q = (const float*)p + at;
+    a = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (n >= 4) {
+      a = *(const f32x4_4*)q;
+    } else if (n > 0) {
+      const float v[3] = {q[0], q[min(1, n - 1)], q[min(2, n - 1)]};
+      a = f32x4{v[0], n > 1 ? v[1] : 0.f, n > 2 ? v[2] : 0.f, 0.f};
+    }
+  }
+  __device__ __forceinline__ f32x4 get() const { return a; }
+  static __device__ __forceinline__ void put(void* p, long long at, int n, f32x4 v) {
+    float* q = (float*)p + at;
+    if (n >= 4) {
+      *(f32x4_4*)q = v;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+        if (i < n) q[i] = v[i];
+    }
+  }
+};
+__device__ __forceinline__ f32x4 four_weights(const void* p, bool bf16, int c, int n) {
+  if (bf16) {
+    Four<true> f;
+    f.load(p, c, n);
+    return f.get();
+  }
+  Four<false> f;
+  f.load(p, c, n);
+  return f.get();
+}
+
+enum { kAfterSum, kGateSum, kBeforeSum, kSums };
+// How many of the columns' sums a launch can take.
+constexpr int sums_of(int U) { return U > 2 ? 2 : 3; }   // (of long rows)
+
+template <int NT, int U, bool H16, bool Y16, bool Z16, bool kY>
 __global__ void __launch_bounds__(NT) join_grad_kernel(JoinArgs a) {
+  constexpr bool kLong = NT == 1024;
   __shared__ float lds[3 * NT / 64];
+  __shared__ f32x4 long_sums[kLong ? sums_of(U) : 1][kLong ? U * NT : 1];
   uint64_t seed = 0, offset = 0;
   if (a.drop) seed = a.rng[0], offset = a.rng[1];
-  const bool norm_x = a.before && a.dz, use_y = a.y && (a.after || a.gate_kind != MOE_GATE_NONE);
-  float sum_after[U][8] = {}, sum_gate[U][8] = {}, sum_before[U][8] = {};
-  for (long long t = blockIdx.x; t < a.T; t += gridDim.x) {
-    const long long row = t * a.H;
-    Raw rd[U], rx[U], rz[U], ry[U];
-    int n[U];
+  const bool norm_x = a.before && a.dz, token = kY && a.gate_kind == MOE_GATE_TOKEN,
+             channel = kY && a.gate_kind == MOE_GATE_CHANNEL, after = kY && a.after;
+  const bool want[kSums] = {after && a.d_after, channel && a.d_gate, norm_x && a.d_before};
+  const int place[kSums] = {0, want[0], want[0] + want[1]};   // of each sum that is wanted
+  const void* const weights[kSums] = {a.after, a.gate, a.before};
+  const bool use[kSums] = {after, channel, norm_x};
+  f32x4 sum[kSums][kLong ? 1 : U] = {}, w[kSums][kLong ? 1 : U] = {};
+  const int c0 = 4 * (int)threadIdx.x;
+  if (kLong) {
+    for (int k = 0; k < sums_of(U); ++k)
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int c = 8 * (u * NT + (int)threadIdx.x);
-      n[u] = min(8, a.H - c);
-      if (norm_x) {
-        rx[u] = load8(a.h, a.h16, row + c, n[u]);
-        rz[u] = load8(a.dz, a.z16, row + c, n[u]);
+      for (int u = 0; u < U; ++u) long_sums[k][u * NT + threadIdx.x] = f32x4{0.f, 0.f, 0.f, 0.f};
+  } else {
+#pragma unroll
+    for (int k = 0; k < kSums; ++k)
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = 4 * NT * u + c0;
+        if (use[k]) w[k][u] = four_weights(weights[k], a.w16, c, a.H - c);
       }
-      if (use_y) ry[u] = load8(a.y, a.y16, row + c, n[u]);
-      if (a.dx) rd[u] = load8(a.dx, a.h16, row + c, n[u]);
+  }
+  auto weight = [&](int k, int u) {
+    const int c = 4 * NT * u + c0;
+    return kLong ? four_weights(weights[k], a.w16, c, a.H - c) : w[k][kLong ? 0 : u];
+  };
+  auto add = [&](int k, int u, f32x4 v) {
+    if (!kLong) sum[k][kLong ? 0 : u] += v;
+    else if (want[k]) long_sums[place[k]][u * NT + threadIdx.x] += v;
+  };
+  struct Rows {   // four of the thread's columns, and the row's gate
+    Four<H16> d, x;
+    Four<Z16> z;
+    Four<Y16> y;
+    float gate;
+  } next[kLong ? 1 : U], now[kLong ? 1 : U];
+  auto load = [&](Rows& o, long long t, int u) {
+    const int c = 4 * NT * u + c0;
+    const long long at = t * a.H + c;
+    if (norm_x) {
+      o.x.load(a.h, at, a.H - c);
+      o.z.load(a.dz, at, a.H - c);
     }
+    if (kY) o.y.load(a.y, at, a.H - c);
+    if (a.dx) o.d.load(a.dx, at, a.H - c);
+    if (token) o.gate = element(a.gate, a.w16, t);
+  };
+  // (a long row's columns come again for each use, by loops that stay loops: unrolled they
+  // take more registers than there are)
+  constexpr int kUnroll = kLong ? 1 : U;
+  auto columns = [&](long long t, int u) -> const Rows& {
+    if (kLong) load(now[0], t, u);
+    return now[kLong ? 0 : u];
+  };
+  auto prefetch = [&](long long t) {
+    if (kLong || t >= a.T) return;
+#pragma unroll
+    for (int u = 0; u < (kLong ? 1 : U); ++u) load(next[u], t, u);
+  };
+  prefetch(blockIdx.x);
+  for (long long t = blockIdx.x; t < a.T; t += gridDim.x) {
+#pragma unroll
+    for (int u = 0; u < (kLong ? 1 : U); ++u) now[u] = next[u];
+    prefetch(t + gridDim.x);
     float s[3] = {0.f, 0.f, 0.f};   // of x^2, x v, y^2
-#pragma unroll
+#pragma unroll kUnroll
     for (int u = 0; u < U; ++u) {
-      const int c = 8 * (u * NT + (int)threadIdx.x);
-      float v[8], w[8], x[8];
+      const Rows& row = columns(t, u);
       if (norm_x) {
-        floats(rx[u], a.h16, x);
-        floats(rz[u], a.z16, v);
-        floats(load8(a.before, a.w16, c, n[u]), a.w16, w);
+        const f32x4 x = row.x.get(), v = row.z.get() * weight(kBeforeSum, u);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 4; ++i) {
           s[0] = fmaf(x[i], x[i], s[0]);
-          s[1] = fmaf(x[i], v[i] * w[i], s[1]);
+          s[1] = fmaf(x[i], v[i], s[1]);
         }
       }
-      if (a.after) {
-        floats(ry[u], a.y16, v);
+      if (after) {
+        const f32x4 y = row.y.get();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[2] = fmaf(v[i], v[i], s[2]);
+        for (int i = 0; i < 4; ++i) s[2] = fmaf(y[i], y[i], s[2]);
       }
     }
     row_sums<NT>(s, lds);
     const float r = rsqrtf(s[0] / a.H + a.eps), m = r * r * (s[1] / a.H);
-    const float q = a.after ? rsqrtf(s[2] / a.H + a.eps) : 1.f;
-    const float gate = use_y && a.gate_kind == MOE_GATE_TOKEN ? element(a.gate, a.w16, t) : 1.f;
-    float d[U][8], s2[2] = {0.f, 0.f};   // of y v of the norm after the block, and da b
-#pragma unroll
+    const float q = after ? rsqrtf(s[2] / a.H + a.eps) : 1.f;
+    f32x4 d[U];
+    float s2[2] = {0.f, 0.f};   // of y v of the norm after the block, and da b
+#pragma unroll kUnroll
     for (int u = 0; u < U; ++u) {
-      const int c = 8 * (u * NT + (int)threadIdx.x);
-      float w[8];
-      if (a.dx)
-        floats(rd[u], a.h16, d[u]);
-      else
-#pragma unroll
-        for (int i = 0; i < 8; ++i) d[u][i] = 0.f;
+      const int c = 4 * NT * u + c0;
+      const long long at = t * a.H + c;
+      const Rows& row = columns(t, u);
+      d[u] = a.dx ? row.d.get() : f32x4{0.f, 0.f, 0.f, 0.f};
       if (norm_x) {
-        float x[8], z[8];
-        floats(rx[u], a.h16, x);
-        floats(rz[u], a.z16, z);
-        floats(load8(a.before, a.w16, c, n[u]), a.w16, w);
+        const f32x4 x = row.x.get(), z = row.z.get(), v = z * weight(kBeforeSum, u);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          d[u][i] = fmaf(r, fmaf(-m, x[i], z[i] * w[i]), d[u][i]);
-          sum_before[u][i] = fmaf(z[i], x[i] * r, sum_before[u][i]);
-        }
+        for (int i = 0; i < 4; ++i) d[u][i] = fmaf(r, fmaf(-m, x[i], v[i]), d[u][i]);
+        add(kBeforeSum, u, z * (x * r));
       }
-      if (a.dh) store8(a.dh, a.h16, row + c, n[u], raw(d[u], a.h16));
-      if (!a.y) continue;
+      if (a.dh) Four<H16>::put(a.dh, at, a.H - c, d[u]);
+      d[u] *= a.scale;
+      if (a.drop) {
+        uint32_t word[4];
+        philox((uint32_t)(c / 4), (uint32_t)t, offset, seed, word);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) d[u][i] *= a.scale;
-      if (a.drop) drop8(a, seed, offset, t, c, d[u]);
-      if (!use_y) continue;
-      float b[8], y[8], wa[8];
-      floats(ry[u], a.y16, y);
-      if (a.after) floats(load8(a.after, a.w16, c, n[u]), a.w16, wa);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) b[i] = a.after ? y[i] * q * wa[i] : y[i];
-      if (a.gate_kind == MOE_GATE_CHANNEL) {
-        floats(load8(a.gate, a.w16, c, n[u]), a.w16, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          sum_gate[u][i] = fmaf(d[u][i], b[i], sum_gate[u][i]);
-          d[u][i] *= w[i];
-        }
-      } else if (a.gate_kind == MOE_GATE_TOKEN) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          s2[1] = fmaf(d[u][i], b[i], s2[1]);
-          d[u][i] *= gate;
-        }
+        for (int i = 0; i < 4; ++i) d[u][i] = word[i] >= a.least ? d[u][i] * a.keep : 0.f;
       }
-      if (a.after) {
+      if (kY) {
+        const f32x4 y = row.y.get(), yn = y * q;
+        const f32x4 wa = after ? weight(kAfterSum, u) : f32x4{1.f, 1.f, 1.f, 1.f}, da = d[u], b = yn * wa;
+        if (channel) {
+          add(kGateSum, u, da * b);
+          d[u] *= weight(kGateSum, u);
+        } else if (token) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          sum_after[u][i] = fmaf(d[u][i], y[i] * q, sum_after[u][i]);
-          d[u][i] *= wa[i];
-          s2[0] = fmaf(d[u][i], y[i], s2[0]);
+          for (int i = 0; i < 4; ++i) s2[1] = fmaf(da[i], b[i], s2[1]);
+          d[u] *= row.gate;
         }
+        if (after) {
+          add(kAfterSum, u, d[u] * yn);
+          d[u] *= wa;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s2[0] = fmaf(d[u][i], y[i], s2[0]);
+        }
+      } else if (a.dy) {
+        Four<Y16>::put(a.dy, at, a.H - c, d[u]);
       }
     }
-    if (!a.y) continue;
+    if (!kY) continue;
     float k = 0.f;
-    if (use_y && (a.after || a.gate_kind == MOE_GATE_TOKEN)) {
+    if (after || token) {
       row_sums<NT>(s2, lds);
-      if (a.gate_kind == MOE_GATE_TOKEN && a.d_gate && threadIdx.x == 0) a.d_gate[t] = s2[1];
+      if (token && a.d_gate && threadIdx.x == 0) a.d_gate[t] = s2[1];
       k = q * q * (s2[0] / a.H);
     }
     if (!a.dy) continue;
-#pragma unroll
+#pragma unroll kUnroll
     for (int u = 0; u < U; ++u) {
-      const int c = 8 * (u * NT + (int)threadIdx.x);
-      if (a.after) {
-        float y[8];
-        floats(ry[u], a.y16, y);
+      const int c = 4 * NT * u + c0;
+      if (after) {
+        if (kLong) now[0].y.load(a.y, t * a.H + c, a.H - c);
+        const f32x4 y = now[kLong ? 0 : u].y.get();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[u][i] = q * fmaf(-k, y[i], d[u][i]);
+        for (int i = 0; i < 4; ++i) d[u][i] = q * fmaf(-k, y[i], d[u][i]);
       }
-      store8(a.dy, a.y16, row + c, n[u], raw(d[u], a.y16));
+      Four<Y16>::put(a.dy, t * a.H + c, a.H - c, d[u]);
     }
   }
   // the columns' sums: this workgroup's part of each, or the whole where it is the only one
-  float* p = a.parts;
-  const long long part = gridDim.x > 1 ? (long long)gridDim.x * a.H : 0;
+  // (a sum that the call has no terms for is zeros)
+  float* const outs[kSums] = {a.d_after, a.gate_kind == MOE_GATE_CHANNEL ? a.d_gate : nullptr, a.d_before};
+  long long skip = 0;
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int c = 8 * (u * NT + (int)threadIdx.x), n = min(8, a.H - c);
-    const long long at = (gridDim.x > 1 ? (long long)blockIdx.x * a.H : 0) + c;
-    long long skip = 0;
-    if (a.d_after) {
-      store8(part ? (void*)(p + skip) : a.d_after, false, at, n, raw(sum_after[u], false));
-      skip += part;
+  for (int k = 0; k < kSums; ++k) {
+    if (!outs[k]) continue;
+    float* const p = gridDim.x > 1 ? a.parts + skip + (long long)blockIdx.x * a.H : outs[k];
+    skip += (long long)gridDim.x * a.H;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int c = 4 * NT * u + c0;
+      const f32x4 v = !kLong ? sum[k][kLong ? 0 : u] : want[k] ? long_sums[place[k]][u * NT + threadIdx.x] : f32x4{0.f, 0.f, 0.f, 0.f};
+      if (c < a.H) Four<false>::put(p, c, a.H - c, v);
     }
-    if (a.d_gate && a.gate_kind == MOE_GATE_CHANNEL) {
-      store8(part ? (void*)(p + skip) : a.d_gate, false, at, n, raw(sum_gate[u], false));
-      skip += part;
-    }
-    if (a.d_before) store8(part ? (void*)(p + skip) : a.d_before, false, at, n, raw(sum_before[u], false));
   }
 }
 
@@ -720,11 +848,21 @@ void with_row(int H, F f) {
   else if (H <= 8192) f(Shape<1024, 1>());
   else f(Shape<1024, 2>());
 }
+template <class F>
+void with_grad_row(int H, F f) {
+  if (H <= 256) f(Shape<64, 1>());
+  else if (H <= 1024) f(Shape<256, 1>());
+  else if (H <= 2048) f(Shape<512, 1>());
+  else if (H <= 4096) f(Shape<512, 2>());
+  else if (H <= 8192) f(Shape<1024, 2>());
+  else f(Shape<1024, 4>());
+}
 // Workgroups of the gradient: enough to fill the card, few enough that their parts are
 // small beside the rows.
 int grad_groups(int T, int H) {
-  const int most = H <= 512 ? 4096 : H <= 2048 ? 1024 : 256;
-  return T < most ? (T < 1 ? 1 : T) : most;
+  const int most = H <= 256 ? 2048 : H <= 1024 ? 1024 : H <= 2048 ? 512 : 256;
+  const int rows = (T + 1) / 2;   // two rows a workgroup, where there are few
+  return rows < most ? (rows < 1 ? 1 : rows) : most;
 }
 
 }  // namespace
@@ -845,12 +983,40 @@ extern "C" int moe_join_grad(const void* dx, const void* dz, const void* x, cons
   }
   if (T == 0) a.drop = false;
   const hipStream_t s = (hipStream_t)stream;
-  with_row(H, [&](auto shape) {
-    constexpr int NT = decltype(shape)::lanes, U = decltype(shape)::each;
-    join_grad_kernel<NT, U><<<(unsigned)G, NT, 0, s>>>(a);
-  });
+  auto launch = [&](const JoinArgs& a) {
+    with_grad_row(H, [&](auto shape) {
+      constexpr int NT = decltype(shape)::lanes, U = decltype(shape)::each;
+      const bool use_y = a.after || a.gate_kind != MOE_GATE_NONE;
+#define MOE_GRAD(H16, Y16, Z16)                                                      \
+  use_y ? join_grad_kernel<NT, U, H16, Y16, Z16, true><<<(unsigned)G, NT, 0, s>>>(a) \
+        : join_grad_kernel<NT, U, H16, Y16, Z16, false><<<(unsigned)G, NT, 0, s>>>(a)
+      switch (4 * a.h16 + 2 * a.y16 + a.z16) {
+        case 0: MOE_GRAD(false, false, false); break;
+        case 1: MOE_GRAD(false, false, true); break;
+        case 2: MOE_GRAD(false, true, false); break;
+        case 3: MOE_GRAD(false, true, true); break;
+        case 4: MOE_GRAD(true, false, false); break;
+        case 5: MOE_GRAD(true, false, true); break;
+        case 6: MOE_GRAD(true, true, false); break;
+        default: MOE_GRAD(true, true, true); break;
+      }
+#undef MOE_GRAD
+    });
+    return hipGetLastError() == hipSuccess;
+  };
+  if (H > 8192 && arrays > 2) {   // LDS holds two of the columns' sums: the third by a launch of its own
+    JoinArgs b = a;
+    b.dx = b.y = b.after = b.gate = nullptr;   // (d_before needs x and dz alone)
+    b.dh = b.dy = nullptr;
+    b.d_after = b.d_gate = nullptr;
+    b.gate_kind = MOE_GATE_NONE;
+    b.drop = false;
+    if (a.parts) b.parts = a.parts + 2LL * G * H;
+    a.d_before = nullptr;
+    if (!launch(b)) return MOE_ERR_HIP;
+  }
+  if (!launch(a)) return MOE_ERR_HIP;
   if (G > 1 && arrays > 0) {
-    if (hipGetLastError() != hipSuccess) return MOE_ERR_HIP;
     float* o[3] = {nullptr, nullptr, nullptr};
     int n = 0;
     if (d_after) o[n++] = d_after;
