@@ -17,7 +17,7 @@ import torch
 
 from . import binding as _b
 from .binding import MoeError, Workspace
-from .experts import (MX4, _FLOAT, _F32, _I32, _MOST, _TYPES, _U8, _BF16, _check, _empty, _mx4_check,
+from .experts import (MX4, _BF16, _F32, _FLOAT, _I32, _MOST, _TYPES, _U8, _check, _empty, _mx4_shapes,
                       _status_word, _stream, _too_large, _two, _written)
 
 EXPORTED = (
@@ -55,15 +55,40 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _place(stream, *tensors):
-    """The handle of the stream to launch on; all of a call is on the current device."""
-    device = torch.cuda.current_device() if _b._raw_device is None else _b._raw_device()
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            raise TypeError(f"expected tensors on the current device ({device}), got one on {t.device}")
+_I64 = (torch.int64,)
+
+
+def _here(stream):
+    """The current device (-2 without one: no tensor is on it) and the handle of the stream
+    to launch on."""
+    if torch.cuda.is_initialized() and _b._raw_device is not None:
+        device = _b._raw_device()
+        if stream is None:
+            return device, _b._raw_stream(device)
+    elif torch.cuda.is_available():
+        device = torch.cuda.current_device()
+    else:
+        return -2, None
     if stream is not None and stream.device_index != device:
         raise TypeError(f"expected a stream of the current device ({device}), got one of {stream.device_index}")
-    return _stream(stream)
+    return device, _stream(stream)
+
+
+def _fits(t, what, shape, dtypes, device):
+    """_check, and that the tensor is on the current device."""
+    if t.get_device() == device and t.dtype in dtypes and t.shape == shape and t.is_contiguous():
+        return
+    _check(t, what, shape, dtypes)
+    raise TypeError(f"{what}: expected a tensor on the current device ({device}), got one on {t.device}")
+
+
+def _matrix(t, what, dtypes, device):
+    """_two, on the current device."""
+    shape = t.shape
+    if t.get_device() == device and len(shape) == 2 and t.dtype in dtypes and t.is_contiguous():
+        return shape
+    _two(t, what, dtypes)
+    raise TypeError(f"{what}: expected a tensor on the current device ({device}), got one on {t.device}")
 
 
 # ---- the router's choice ---------------------------------------------------------------
@@ -87,20 +112,20 @@ def choose(logits, topk: int, bias=None, score: str = "softmax", renormalize: bo
     logits + bias (fp32 [E]; it acts on the choice alone), ties to the lower index,
     and their gates: scale times the score (softmax over all experts, or sigmoid),
     renormalised over the chosen or not.  Logits of -inf are never chosen."""
-    T, E = _two(logits, "logits", _FLOAT)
+    L, (device, handle) = lib(), _here(stream)
+    T, E = _matrix(logits, "logits", _FLOAT, device)
     if (T | E | topk) > _MOST:
         _too_large("moe_choose")
     if bias is not None:
-        _check(bias, "bias", (E,), _F32)
+        _fits(bias, "bias", (E,), _F32, device)
     given, shape = out, (T, topk)
-    L = lib()
     if out is None:
         out = Choice(_empty(shape, torch.int32, logits.device, stream), _empty(shape, torch.float32, logits.device, stream))
     else:
-        _check(out[0], "expert_ids", shape, _I32)
-        _check(out[1], "gates", shape, _F32)
+        _fits(out[0], "expert_ids", shape, _I32, device)
+        _fits(out[1], "gates", shape, _F32, device)
     r = L.moe_choose(logits.data_ptr(), _ptr(bias), out[0].data_ptr(), out[1].data_ptr(), T, E, topk,
-                     _TYPES[logits.dtype], _score(score), renormalize, scale, _place(stream, logits, bias, *out))
+                     _TYPES[logits.dtype], _score(score), renormalize, scale, handle)
     if r < 0:
         raise MoeError(r, "moe_choose")
     if given is not None:
@@ -112,20 +137,22 @@ def choose_grad(d_gates, logits, expert_ids, score: str = "softmax", renormalize
                 out=None, workspace: Optional[Workspace] = None, stream=None):
     """moe_choose_grad: the gates' gradient fp32 [T, topk], the logits and the chosen
     ids to the logits' gradient [T, E], of their type."""
-    T, E = shape = _two(logits, "logits", _FLOAT)
-    topk = _two(expert_ids, "expert_ids", _I32)[1]
+    L, (device, handle) = lib(), _here(stream)
+    T, E = shape = _matrix(logits, "logits", _FLOAT, device)
+    chosen = _matrix(expert_ids, "expert_ids", _I32, device)
+    topk = chosen[1]
+    if chosen[0] != T:
+        raise TypeError(f"expert_ids: {chosen[0]} tokens, logits {T}")
     if (T | E | topk) > _MOST:
         _too_large("moe_choose_grad")
-    _check(expert_ids, "expert_ids", (T, topk), _I32)
-    _check(d_gates, "d_gates", (T, topk), _F32)
+    _fits(d_gates, "d_gates", chosen, _F32, device)
     given = out
     if out is None:
         out = _empty(shape, logits.dtype, logits.device, stream)
     else:
-        _check(out, "out", shape, (logits.dtype,))
-    r = lib().moe_choose_grad(d_gates.data_ptr(), logits.data_ptr(), expert_ids.data_ptr(), out.data_ptr(), T, E, topk,
-                              _TYPES[logits.dtype], _score(score), renormalize, scale, _status_word(workspace),
-                              _place(stream, d_gates, logits, expert_ids, out))
+        _fits(out, "out", shape, (logits.dtype,), device)
+    r = L.moe_choose_grad(d_gates.data_ptr(), logits.data_ptr(), expert_ids.data_ptr(), out.data_ptr(), T, E, topk,
+                          _TYPES[logits.dtype], _score(score), renormalize, scale, _status_word(workspace), handle)
     if r < 0:
         raise MoeError(r, "moe_choose_grad")
     if given is not None:
@@ -152,30 +179,32 @@ class JoinGrads(NamedTuple):
     before: Optional[torch.Tensor]
 
 
-def _weights(T, H, after, gate, before):
+def _weights(T, H, after, gate, before, device):
     """The kind of gate and the type that norms' weights and the gate share."""
-    dtype = None
-    for what, t in (("after", after), ("before", before)):
-        if t is not None:
-            dtype = dtype or t.dtype
-            _check(t, what, (H,), _FLOAT if dtype in _FLOAT and dtype == t.dtype else (dtype,))
+    types = _FLOAT
+    if after is not None:
+        _fits(after, "after", (H,), types, device)
+        types = (after.dtype,)
+    if before is not None:
+        _fits(before, "before", (H,), types, device)
+        types = (before.dtype,)
     kind = _NONE
     if gate is not None:
-        dtype = dtype or gate.dtype
         kind = _CHANNEL if gate.shape == (1, H) else _TOKEN
-        _check(gate, "gate", (1, H) if kind == _CHANNEL else (T, 1), (dtype,) if dtype in _FLOAT else _FLOAT)
-    return kind, _TYPES[dtype] if dtype is not None else 1
+        _fits(gate, "gate", (1, H) if kind == _CHANNEL else (T, 1), types, device)
+        types = (gate.dtype,)
+    return kind, _TYPES[types[0]]
 
 
-def _rng(rng, drop):
+def _rng(rng, drop, device):
+    if drop == 0.0:
+        return None
     if not 0.0 <= drop < 1.0:
         raise ValueError(f"drop: expected a probability below 1, got {drop}")
-    if drop > 0.0:
-        if rng is None:
-            raise TypeError("rng: dropout needs one, int64 [2] (seed, offset)")
-        _check(rng, "rng", (2,), (torch.int64,))
-        return rng.data_ptr()
-    return None
+    if rng is None:
+        raise TypeError("rng: dropout needs one, int64 [2] (seed, offset)")
+    _fits(rng, "rng", (2,), _I64, device)
+    return rng.data_ptr()
 
 
 def join(h, y=None, after=None, gate=None, scale: float = 1.0, drop: float = 0.0, rng=None, before=None,
@@ -192,28 +221,28 @@ def join(h, y=None, after=None, gate=None, scale: float = 1.0, drop: float = 0.0
     out: where both go (out.h may be h itself; out.z None without `before`)."""
     if h is None and y is None:
         raise TypeError("expected h, y or both")
+    L, (device, handle) = lib(), _here(stream)
     some = h if h is not None else y
-    T, H = shape = _two(some, "h" if h is not None else "y", _FLOAT)
+    T, H = shape = _matrix(some, "h" if h is not None else "y", _FLOAT, device)
     if (T | H) > _MOST:
         _too_large("moe_join")
     if y is not None and h is not None:
-        _check(y, "y", shape, _FLOAT)
-    kind, w_type = _weights(T, H, after, gate, before)
-    seeds, given, L = _rng(rng, drop), out, lib()
+        _fits(y, "y", shape, _FLOAT, device)
+    kind, w_type = _weights(T, H, after, gate, before, device)
+    seeds, given, h_type = _rng(rng, drop, device), out, some.dtype
     if out is None:
-        x = h if y is None else _empty(shape, some.dtype, some.device, stream)
+        x = h if y is None else _empty(shape, h_type, some.device, stream)
         z = None if before is None else _empty(shape, dtype, some.device, stream)
         out = Joined(x, z)
     x, z = out
     if y is not None:
-        _check(x, "out.h", shape, (some.dtype,))
+        _fits(x, "out.h", shape, (h_type,), device)
     if before is not None:
-        _check(z, "out.z", shape, _FLOAT)
+        _fits(z, "out.z", shape, _FLOAT, device)
     r = L.moe_join(_ptr(h), _ptr(y), _ptr(after), _ptr(gate), _ptr(before), seeds,
                    None if y is None else x.data_ptr(), None if before is None else z.data_ptr(), T, H,
-                   _TYPES[some.dtype], 0 if y is None else _TYPES[y.dtype], 0 if before is None else _TYPES[z.dtype],
-                   w_type, kind, scale, drop, eps,
-                   _place(stream, h, y, after, gate, before, rng if seeds else None, x, z if before is not None else None))
+                   _TYPES[h_type], 0 if y is None else _TYPES[y.dtype], 0 if before is None else _TYPES[z.dtype],
+                   w_type, kind, scale, drop, eps, handle)
     if r < 0:
         raise MoeError(r, "moe_join")
     if given is not None:
@@ -239,51 +268,56 @@ def join_grad(d_h, d_z, h, y=None, after=None, gate=None, scale: float = 1.0, dr
     some = d_h if d_h is not None else h
     if some is None:
         raise TypeError("expected d_h, or d_z and h")
-    T, H = shape = _two(some, "d_h" if d_h is not None else "h", _FLOAT)
+    L, (device, handle) = lib(), _here(stream)
+    T, H = shape = _matrix(some, "d_h" if d_h is not None else "h", _FLOAT, device)
     if (T | H) > _MOST:
         _too_large("moe_join_grad")
     dtype, dev = some.dtype, some.device
     if d_z is not None:
         if before is None or h is None:
             raise TypeError("d_z: expected `before` and h with it")
-        _check(h, "h", shape, (dtype,))
-        _check(d_z, "d_z", shape, _FLOAT)
+        if h is not some:
+            _fits(h, "h", shape, (dtype,), device)
+        _fits(d_z, "d_z", shape, _FLOAT, device)
+    elif d_h is None:
+        raise TypeError("expected d_h, d_z or both")
     if y is not None:
-        _check(y, "y", shape, _FLOAT)
-    kind, w_type = _weights(T, H, after, gate, before)
-    seeds, L = _rng(rng, drop), lib()
+        _fits(y, "y", shape, _FLOAT, device)
+    kind, w_type = _weights(T, H, after, gate, before, device)
+    seeds, given = _rng(rng, drop, device), out
     if out is None:
         f32 = torch.float32
-        given = None
         out = JoinGrads(_empty(shape, dtype, dev, stream) if residual else None,
                         _empty(shape, y.dtype, dev, stream) if y is not None else None,
                         _empty((H,), f32, dev, stream) if after is not None else None,
                         _empty(gate.shape, f32, dev, stream) if gate is not None else None,
                         _empty((H,), f32, dev, stream) if before is not None else None)
-    else:
-        given = out
-        for what, t, s, types in (("out.h", out.h, shape, (dtype,)), ("out.y", out.y, shape, (y.dtype,) if y is not None else ()),
-                                  ("out.after", out.after, (H,), _F32),
-                                  ("out.gate", out.gate, gate.shape if gate is not None else (), _F32),
-                                  ("out.before", out.before, (H,), _F32)):
-            if t is not None:
-                _check(t, what, s, types)
-    if scratch is None and (out.after is not None or out.before is not None or (out.gate is not None and kind == _CHANNEL)):
+    g_h, g_y, g_after, g_gate, g_before = out
+    if given is not None:
+        if g_h is not None:
+            _fits(g_h, "out.h", shape, (dtype,), device)
+        if g_y is not None:
+            _fits(g_y, "out.y", shape, (y.dtype,) if y is not None else (), device)
+        if g_after is not None:
+            _fits(g_after, "out.after", (H,), _F32, device)
+        if g_gate is not None:
+            _fits(g_gate, "out.gate", gate.shape if gate is not None else (), _F32, device)
+        if g_before is not None:
+            _fits(g_before, "out.before", (H,), _F32, device)
+    if scratch is None and (g_after is not None or g_before is not None or (g_gate is not None and kind == _CHANNEL)):
         scratch = _empty((L.moe_join_grad_scratch_size(T, H),), torch.uint8, dev, stream)
     room = 0
     if scratch is not None:
-        _check(scratch, "scratch", scratch.shape, _U8)
+        _fits(scratch, "scratch", scratch.shape, _U8, device)
         room = scratch.numel()
-    r = L.moe_join_grad(_ptr(d_h), _ptr(d_z), _ptr(h) if d_z is not None else None, _ptr(y), _ptr(after), _ptr(gate),
-                        _ptr(before), seeds, _ptr(out.h), _ptr(out.y), _ptr(out.after), _ptr(out.gate), _ptr(out.before),
+    r = L.moe_join_grad(_ptr(d_h), _ptr(d_z), None if d_z is None else h.data_ptr(), _ptr(y), _ptr(after), _ptr(gate),
+                        _ptr(before), seeds, _ptr(g_h), _ptr(g_y), _ptr(g_after), _ptr(g_gate), _ptr(g_before),
                         T, H, _TYPES[dtype], 0 if y is None else _TYPES[y.dtype], 0 if d_z is None else _TYPES[d_z.dtype],
-                        w_type, kind, scale, drop, eps, scratch.data_ptr() if room else None, room,
-                        _place(stream, d_h, d_z, h if d_z is not None else None, y, after, gate, before,
-                               rng if seeds else None, scratch, *out))
+                        w_type, kind, scale, drop, eps, scratch.data_ptr() if room else None, room, handle)
     if r < 0:
         raise MoeError(r, "moe_join_grad")
     if given is not None:
-        _written(tuple(t for t in given if t is not None))
+        _written(tuple([t for t in given if t is not None]))
     return out
 
 
@@ -302,47 +336,53 @@ def layer_few(hidden, w1, w2, expert_ids, gates, first_expert: int = 0, out=None
     gates fp32 [T, topk] (ids outside [first_expert, first_expert + E): no expert); returns
     out [T, H] (`dtype`: fp32 or bf16).  scratch: uint8, at least
     layer_few_scratch_size bytes (allocated if None)."""
-    T, H = _two(hidden, "hidden", _BF16)
-    shape = _two(expert_ids, "expert_ids", _I32)
+    L, (device, handle) = lib(), _here(stream)
+    T, H = _matrix(hidden, "hidden", _BF16, device)
+    shape = _matrix(expert_ids, "expert_ids", _I32, device)
     topk = shape[1]
     if shape[0] != T:
         raise TypeError(f"expert_ids: {shape[0]} tokens, hidden {T}")
-    _check(gates, "gates", shape, _F32)
+    _fits(gates, "gates", shape, _F32, device)
     mx4 = isinstance(w1, MX4)
     if mx4 != isinstance(w2, MX4):
         raise TypeError("w1 and w2: expected both in bf16 or both in MX4")
     if mx4:
-        if len(w1.codes.shape) != 3 or w1.codes.shape[1] % 2 or w1.K != H:
-            raise TypeError(f"w1: expected [E, 2I, {H}] in MX4, got {tuple(w1.codes.shape)}, K = {w1.K}")
-        E, I = w1.codes.shape[0], w1.codes.shape[1] // 2
-        _mx4_check(w1, "w1", (E, 2 * I))
-        if w2.K != I:
-            raise TypeError(f"w2: K is {w2.K}, expected {I}")
-        _mx4_check(w2, "w2", (E, H))
+        (c1, s1, K1), (c2, s2, K2) = w1, w2
+        if len(c1.shape) != 3 or c1.shape[1] % 2 or K1 != H:
+            raise TypeError(f"w1: expected [E, 2I, {H}] in MX4, got {tuple(c1.shape)}, K = {K1}")
+        E, N = c1.shape[:2]
+        I = N // 2
+        if K2 != I:
+            raise TypeError(f"w2: K is {K2}, expected {I}")
+        codes, scales = _mx4_shapes((E, N), H)
+        _fits(c1, "w1.codes", codes, _U8, device)
+        _fits(s1, "w1.scales", scales, _U8, device)
+        codes, scales = _mx4_shapes((E, H), I)
+        _fits(c2, "w2.codes", codes, _U8, device)
+        _fits(s2, "w2.scales", scales, _U8, device)
     else:
         if w2.dim() != 3:
             raise TypeError(f"w2: expected [E, I, H], got {tuple(w2.shape)}")
         E, I = w2.shape[:2]
-        _check(w1, "w1", (E, H, 2 * I), _BF16)
-        _check(w2, "w2", (E, I, H), _BF16)
+        _fits(w1, "w1", (E, H, 2 * I), _BF16, device)
+        _fits(w2, "w2", (E, I, H), _BF16, device)
     if (T | H | I | E | topk) > _MOST or not -_MOST <= first_expert + 1 <= _MOST + 1:
         _too_large("layer_few")
     given = out
     if out is None:
         out = _empty((T, H), dtype, hidden.device, stream)
-    _check(out, "out", (T, H), _FLOAT)
-    L = lib()
+    _fits(out, "out", (T, H), _FLOAT, device)
     if scratch is None:
         scratch = _empty((L.moe_few_scratch_size(T, H, I, E, topk),), torch.uint8, hidden.device, stream)
-    _check(scratch, "scratch", scratch.shape, _U8)
-    rest = (expert_ids.data_ptr(), gates.data_ptr(), out.data_ptr(), T, H, I, E, topk, first_expert, _TYPES[out.dtype],
-            scratch.data_ptr(), scratch.numel(),
-            _place(stream, hidden, *(w1[:2] + w2[:2] if mx4 else (w1, w2)), expert_ids, gates, out, scratch))
+    _fits(scratch, "scratch", scratch.shape, _U8, device)
     if mx4:
-        r = L.moe_few_forward_mx4(hidden.data_ptr(), w1.codes.data_ptr(), w1.scales.data_ptr(), w2.codes.data_ptr(),
-                                  w2.scales.data_ptr(), *rest)
+        r = L.moe_few_forward_mx4(hidden.data_ptr(), c1.data_ptr(), s1.data_ptr(), c2.data_ptr(), s2.data_ptr(),
+                                  expert_ids.data_ptr(), gates.data_ptr(), out.data_ptr(), T, H, I, E, topk, first_expert,
+                                  _TYPES[out.dtype], scratch.data_ptr(), scratch.numel(), handle)
     else:
-        r = L.moe_few_forward(hidden.data_ptr(), w1.data_ptr(), w2.data_ptr(), *rest)
+        r = L.moe_few_forward(hidden.data_ptr(), w1.data_ptr(), w2.data_ptr(), expert_ids.data_ptr(), gates.data_ptr(),
+                              out.data_ptr(), T, H, I, E, topk, first_expert, _TYPES[out.dtype], scratch.data_ptr(),
+                              scratch.numel(), handle)
     if r < 0:
         raise MoeError(r, "layer_few")
     if given is not None:
