@@ -56,6 +56,7 @@ __device__ __forceinline__ int min_of(int v) {
 // holds experts 4 (q L + l) + i.  A slot is the group's largest key, then the lowest
 // expert that has it; its lane notes the slot and strikes the key out.
 constexpr float kNone = -__builtin_inff();
+constexpr int kMaxTopk = 64, kMaxExperts = 1024;
 
 template <class T, int L, int R>
 __device__ __forceinline__ void load_logits(const T* p, int E, int l, float (&v)[R]) {
@@ -83,88 +84,90 @@ __device__ __forceinline__ int ordered(float v) {
 }
 __device__ __forceinline__ float unordered(int k) { return __int_as_float(k ^ ((k >> 31) & 0x7fffffff)); }
 
-// Bound by the instructions of the rounds (two comparisons and two selections for each
-// logit of a lane): 16384 tokens, 8 of 256 experts, by sixteen lanes a token.  The scores are
-// taken of the chosen alone, spread over the lanes: slot j is lane j % L's.
+// Bound by the instructions of the rounds: for each logit of a lane two comparisons and two
+// selections (16384 tokens, 8 of 256 experts by sixteen lanes a token: 10.8 us, of which
+// the launch and 18 MB are some 5; by eight lanes 11.2; a threshold found bit by bit over a
+// wave's counts 15).  The chosen go through LDS to the lanes that take their scores: slot
+// j is lane j % L's.
 template <class T, int L, int R>
 __global__ void __launch_bounds__(256) choose_kernel(const T* logits, const float* bias, int32_t* ids, float* gates,
                                                      long long first, int tokens, int E, int topk, bool softmax,
                                                      bool renorm, float scale) {
-  constexpr int S = L == 64 ? 1 : 4;   // slots of a lane
-  const int l = threadIdx.x % L;
-  const long long t0 = first + (long long)blockIdx.x * (256 / L) + threadIdx.x / L;
-  const bool in = t0 < tokens;
+  __shared__ int32_t lds_id[256 / L][kMaxTopk];
+  __shared__ float lds_x[256 / L][kMaxTopk];
+  const int l = threadIdx.x % L, group = threadIdx.x / L;
+  const long long t0 = first + (long long)blockIdx.x * (256 / L) + group;
+  const bool in = t0 < tokens, all = softmax && !renorm;
   const long long t = in ? t0 : tokens - 1;   // (groups past the last token do its work again, and write nothing)
   float v[R], b[R];
   load_logits<T, L, R>(logits + t * E, E, l, v);
   if (bias) load_logits<float, L, R>(bias, E, l, b);
+  float shift = kNone, sum = 0.f;
+  if (all) {   // (kNone, which is past E too, adds nothing)
+#pragma unroll
+    for (int r = 0; r < R; ++r) shift = fmaxf(shift, v[r]);
+    shift = max_of<L>(shift);
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (v[r] != kNone) sum += expf(v[r] - shift);
+  }
   const int none = ordered(kNone);
   int key[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const float k = bias ? v[r] + b[r] : v[r] + 0.f;   // (+ 0: -0 and 0 are equal)
-    key[r] = k > kNone ? ordered(k + 0.f) : none;      // (past E: kNone)
+    const float k = (bias ? v[r] + b[r] : v[r]) + 0.f;   // (+ 0: -0 and 0 are equal)
+    key[r] = k > kNone ? ordered(k) : none;
   }
-  int id[S];
-  float chosen[S];
-#pragma unroll
-  for (int s = 0; s < S; ++s) id[s] = -1, chosen[s] = kNone;
+  for (int j = l; j < topk; j += L) lds_id[group][j] = -1;
   for (int n = 0; n < topk; ++n) {
     int best = key[0];
 #pragma unroll
     for (int r = 1; r < R; ++r) best = max(best, key[r]);
     best = over_lanes<L>(best, [](int x, int y) { return max(x, y); });
-    if (__ballot(best > none) == 0) break;   // no token of the wave has another
+    const uint64_t live = __ballot(best > none);
+    if (live == 0) break;   // no token of the wave has another
     int e = INT32_MAX;
 #pragma unroll
     for (int r = R - 1; r >= 0; --r) e = key[r] == best ? 4 * (r / 4 * L + l) + r % 4 : e;
-    e = min_of<L>(best > none ? e : INT32_MAX);
-    float x = kNone;
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const bool it = e == 4 * (r / 4 * L + l) + r % 4;
-      key[r] = it ? none : key[r];
-      if (bias) x = it ? v[r] : x;
+    e = best > none ? e : INT32_MAX;
+    // more lanes than tokens have it: equal keys, of which the lower expert's goes first
+    if (__popcll(__ballot(e != INT32_MAX)) * L != __popcll(live)) {
+      const int least = min_of<L>(e);
+      e = e == least ? e : INT32_MAX;
     }
-    x = bias ? max_of<L>(x) : unordered(best);
+    if (e != INT32_MAX) lds_id[group][n] = e;
 #pragma unroll
-    for (int s = 0; s < S; ++s)
-      if (n == s * L + l && best > none) id[s] = e, chosen[s] = x;
+    for (int r = 0; r < R; ++r) key[r] = e == 4 * (r / 4 * L + l) + r % 4 ? none : key[r];
   }
-  const bool all = softmax && !renorm;
-  float shift = kNone, sum = 0.f, p[S];
-  if (all) {
-#pragma unroll
-    for (int r = 0; r < R; ++r) shift = fmaxf(shift, v[r]);
-  } else {
-#pragma unroll
-    for (int s = 0; s < S; ++s) shift = fmaxf(shift, softmax ? chosen[s] : fminf(chosen[s], 0.f));
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (a wave reads what it wrote)
+  if (!all) {
+    for (int j = l; j < topk; j += L) {
+      const int e = lds_id[group][j];
+      const float x = e < 0 ? kNone : (float)logits[t * E + e];
+      lds_x[group][j] = x;
+      shift = fmaxf(shift, softmax ? x : fminf(x, 0.f));
+    }
+    shift = max_of<L>(shift);
   }
-  shift = max_of<L>(shift);
-#pragma unroll
-  for (int s = 0; s < S; ++s) {
-    p[s] = 0.f;
-    if (id[s] < 0) continue;
+  for (int j = l; j < topk; j += L) {
+    const int e = lds_id[group][j];
+    const float x = !all ? lds_x[group][j] : e < 0 ? kNone : (float)logits[t * E + e];
     // (renormalised sigmoids by their ratio to the largest: none is lost to underflow)
-    p[s] = softmax ? expf(chosen[s] - shift)
-           : renorm ? expf(fminf(chosen[s], 0.f) - shift) / (1.f + expf(-fabsf(chosen[s])))
-                    : sigmoid(chosen[s]);
-    if (renorm) sum += p[s];
-  }
-  if (all) {
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-      if (4 * (r / 4 * L + l) + r % 4 < E) sum += expf(v[r] - shift);
+    const float p = e < 0     ? 0.f
+        : softmax ? expf(x - shift)
+        : renorm  ? expf(fminf(x, 0.f) - shift) / (1.f + expf(-fabsf(x)))
+                  : sigmoid(x);
+    if (renorm) sum += p;
+    lds_x[group][j] = p;
   }
   sum = sum_of<L>(sum);
   const float f = softmax || renorm ? scale / sum : scale;
   if (!in) return;
-#pragma unroll
-  for (int s = 0; s < S; ++s)
-    if (s * L + l < topk) {
-      ids[t * topk + s * L + l] = id[s];
-      gates[t * topk + s * L + l] = id[s] < 0 ? 0.f : p[s] * f;
-    }
+  for (int j = l; j < topk; j += L) {
+    const int e = lds_id[group][j];
+    ids[t * topk + j] = e;
+    gates[t * topk + j] = e < 0 ? 0.f : lds_x[group][j] * f;
+  }
 }
 
 // With q_j the gates over `scale`, the chosen slots' gradients g_j, and G = sum q_j g_j:
@@ -268,39 +271,49 @@ typedef uint32_t u32x4_4 __attribute__((ext_vector_type(4), aligned(4)));
 struct Raw {
   u32x4 a, b;
 };
-// n: how many of the eight exist (the others are zeros)
-__device__ __forceinline__ Raw load8(const void* p, bool bf16, long long at, int n) {
+// Columns c .. c + 7 of a row of H that starts at element `row`, zeros past its end.  The
+// lanes at the end of a row load its last eight, and floats() shifts them down: single
+// elements in a branch of their own make the wave wait there, tensor after tensor, and a
+// shift right after the load makes it wait for that.  Rows of fewer than eight are left to
+// floats().
+__device__ __forceinline__ Raw load8(const void* p, bool bf16, long long row, int c, int H) {
   Raw r = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-  if (n >= 8) {
+  const int at = min(c, H - 8);
+  if (c - at < 8 && at >= 0) {
     if (bf16) {
-      r.a = *(const u32x4_2*)((const uint16_t*)p + at);
+      r.a = *(const u32x4_2*)((const uint16_t*)p + row + at);
     } else {
-      r.a = *(const u32x4_4*)((const uint32_t*)p + at);
-      r.b = *(const u32x4_4*)((const uint32_t*)p + at + 4);
-    }
-  } else if (n > 0) {   // (the last one again instead of those past the end: no load waits for a test)
-    if (bf16) {
-      const uint16_t* q = (const uint16_t*)p + at;
-      uint32_t v[7];
-#pragma unroll
-      for (int i = 0; i < 7; ++i) v[i] = q[min(i, n - 1)];
-#pragma unroll
-      for (int i = 0; i < 7; ++i) r.a[i / 2] |= i < n ? v[i] << (16 * (i % 2)) : 0;
-    } else {
-      const uint32_t* q = (const uint32_t*)p + at;
-      uint32_t v[7];
-#pragma unroll
-      for (int i = 0; i < 7; ++i) v[i] = q[min(i, n - 1)];
-#pragma unroll
-      for (int i = 0; i < 7; ++i) {
-        if (i < 4) r.a[i % 4] = i < n ? v[i] : 0;
-        else r.b[i % 4] = i < n ? v[i] : 0;
-      }
+      r.a = *(const u32x4_4*)((const uint32_t*)p + row + at);
+      r.b = *(const u32x4_4*)((const uint32_t*)p + row + at + 4);
     }
   }
   return r;
 }
-__device__ __forceinline__ void floats(const Raw& r, bool bf16, float (&v)[8]) {
+// the same as floats, from what load8 gave for them
+__device__ __forceinline__ void floats(Raw r, bool bf16, const void* p, long long row, int c, int H, float (&v)[8]) {
+  if (H % 8) {   // (uniform)
+    const int s = c - min(c, H - 8);
+    if (H < 8) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        v[i] = i >= H - c ? 0.f
+               : bf16     ? __uint_as_float((uint32_t)((const uint16_t*)p)[row + c + i] << 16)
+                          : ((const float*)p)[row + c + i];
+      return;
+    }
+    if (bf16) {
+      if (s & 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.a[i] = r.a[i] >> 16 | (i < 3 ? r.a[(i + 1) % 4] << 16 : 0);
+      }
+      if (s & 2) r.a = u32x4{r.a[1], r.a[2], r.a[3], 0};
+      if (s & 4) r.a = u32x4{r.a[2], r.a[3], 0, 0};
+    } else {
+      if (s & 1) r.a = u32x4{r.a[1], r.a[2], r.a[3], r.b[0]}, r.b = u32x4{r.b[1], r.b[2], r.b[3], 0};
+      if (s & 2) r.a = u32x4{r.a[2], r.a[3], r.b[0], r.b[1]}, r.b = u32x4{r.b[2], r.b[3], 0, 0};
+      if (s & 4) r.a = r.b, r.b = u32x4{0, 0, 0, 0};
+    }
+  }
   if (bf16) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -311,6 +324,9 @@ __device__ __forceinline__ void floats(const Raw& r, bool bf16, float (&v)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(i < 4 ? r.a[i % 4] : r.b[i % 4]);
   }
+}
+__device__ __forceinline__ void floats_of(const void* p, bool bf16, int c, int H, float (&v)[8]) {
+  floats(load8(p, bf16, 0, c, H), bf16, p, 0, c, H, v);
 }
 __device__ __forceinline__ Raw raw(const float (&v)[8], bool bf16) {
   Raw r;
@@ -396,13 +412,13 @@ __device__ __forceinline__ void drop8(const JoinArgs& a, uint64_t seed, uint64_t
   }
 }
 
-// Sums of n values over the NT threads of a row; rows of a workgroup use LDS of their own.
+// Sums of n values over a row's threads: NT, or as many waves fewer as its columns need.
 template <int NT, int n>
 __device__ __forceinline__ void row_sums(float (&v)[n], float* lds) {
 #pragma unroll
   for (int i = 0; i < n; ++i) v[i] = sum_of<64>(v[i]);
   if (NT == 64) return;
-  const int wave = threadIdx.x / 64;
+  const int wave = threadIdx.x / 64, waves = blockDim.x / 64;
   __syncthreads();   // (the last sums have been read)
   if (threadIdx.x % 64 == 0) {
 #pragma unroll
@@ -413,7 +429,7 @@ __device__ __forceinline__ void row_sums(float (&v)[n], float* lds) {
   for (int i = 0; i < n; ++i) {
     float s = 0.f;
 #pragma unroll
-    for (int w = 0; w < NT / 64; ++w) s += lds[i * (NT / 64) + w];
+    for (int w = 0; w < NT / 64; ++w) s += w < waves ? lds[i * (NT / 64) + w] : 0.f;
     v[i] = s;
   }
 }
@@ -431,8 +447,8 @@ __global__ void __launch_bounds__(NT) join_kernel(JoinArgs a, long long first) {
   for (int u = 0; u < U; ++u) {
     const int c = 8 * (u * NT + (int)threadIdx.x);
     n[u] = min(8, a.H - c);
-    if (a.y) ry[u] = load8(a.y, a.y16, row + c, n[u]);
-    if (a.h) rh[u] = load8(a.h, a.h16, row + c, n[u]);
+    if (a.y) ry[u] = load8(a.y, a.y16, row, c, a.H);
+    if (a.h) rh[u] = load8(a.h, a.h16, row, c, a.H);
   }
   if (a.drop) seed = a.rng[0], offset = a.rng[1];
   float factor = a.scale;
@@ -443,7 +459,7 @@ __global__ void __launch_bounds__(NT) join_kernel(JoinArgs a, long long first) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       float y[8];
-      floats(ry[u], a.y16, y);
+      floats(ry[u], a.y16, a.y, row, 8 * (u * NT + (int)threadIdx.x), a.H, y);
 #pragma unroll
       for (int i = 0; i < 8; ++i) s[0] = fmaf(y[i], y[i], s[0]);
     }
@@ -455,20 +471,20 @@ __global__ void __launch_bounds__(NT) join_kernel(JoinArgs a, long long first) {
   for (int u = 0; u < U; ++u) {
     const int c = 8 * (u * NT + (int)threadIdx.x);
     if (a.h)
-      floats(rh[u], a.h16, x[u]);
+      floats(rh[u], a.h16, a.h, row, c, a.H, x[u]);
     else
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[u][i] = 0.f;
     if (a.y) {
       float v[8], w[8];
-      floats(ry[u], a.y16, v);
+      floats(ry[u], a.y16, a.y, row, c, a.H, v);
       if (a.after) {
-        floats(load8(a.after, a.w16, c, n[u]), a.w16, w);
+        floats_of(a.after, a.w16, c, a.H, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = v[i] * r * w[i];
       }
       if (a.gate_kind == MOE_GATE_CHANNEL) {
-        floats(load8(a.gate, a.w16, c, n[u]), a.w16, w);
+        floats_of(a.gate, a.w16, c, a.H, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] *= w[i];
       }
@@ -477,7 +493,10 @@ __global__ void __launch_bounds__(NT) join_kernel(JoinArgs a, long long first) {
       for (int i = 0; i < 8; ++i) x[u][i] = fmaf(factor, v[i], x[u][i]);
       const Raw o = raw(x[u], a.h16);
       store8(a.x, a.h16, row + c, n[u], o);
-      floats(o, a.h16, x[u]);   // the norm's x is the one that is kept
+      if (a.h16) {   // the norm's x is the one that is kept
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[u][i] = __uint_as_float(i % 2 ? o.a[i / 2] & 0xffff0000u : o.a[i / 2] << 16);
+      }
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) s[0] = fmaf(x[u][i], x[u][i], s[0]);
@@ -489,7 +508,7 @@ __global__ void __launch_bounds__(NT) join_kernel(JoinArgs a, long long first) {
   for (int u = 0; u < U; ++u) {
     const int c = 8 * (u * NT + (int)threadIdx.x);
     float w[8];
-    floats(load8(a.before, a.w16, c, n[u]), a.w16, w);
+    floats_of(a.before, a.w16, c, a.H, w);
 #pragma unroll
     for (int i = 0; i < 8; ++i) w[i] *= x[u][i] * r;
     store8(a.z, a.z16, row + c, n[u], raw(w, a.z16));
@@ -513,15 +532,24 @@ struct Four<true> {
   typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
   typedef uint32_t u32x2_2 __attribute__((ext_vector_type(2), aligned(2)));
   u32x2 a;
-  __device__ __forceinline__ void load(const void* p, long long at, int n) {
-    const uint16_t* q = (const uint16_t*)p + at;
+  // columns c .. c + 3 of a row that starts at element `row`, as load8 and floats do it
+  __device__ __forceinline__ void load(const void* p, long long row, int c, int H) {
+    const int at = min(c, H - 4);
     a = u32x2{0, 0};
-    if (n >= 4) {
-      a = *(const u32x2_2*)q;
-    } else if (n > 0) {
-      const uint32_t v[3] = {q[0], q[min(1, n - 1)], q[min(2, n - 1)]};
-      a = u32x2{v[0] | (n > 1 ? v[1] << 16 : 0), n > 2 ? v[2] : 0};
+    if (c - at < 4 && at >= 0) a = *(const u32x2_2*)((const uint16_t*)p + row + at);
+  }
+  // (where the row's end is no multiple of four; the loads have to be there)
+  __device__ __forceinline__ void settle(const void* p, long long row, int c, int H) {
+    uint64_t v = (uint64_t)a[1] << 32 | a[0];
+    if (H < 4) {
+      v = 0;
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+        if (i < H - c) v |= (uint64_t)((const uint16_t*)p)[row + c + i] << (16 * i);
+    } else {
+      v >>= 16 * ((c - min(c, H - 4)) & 3);
     }
+    a = u32x2{(uint32_t)v, (uint32_t)(v >> 32)};
   }
   __device__ __forceinline__ f32x4 get() const {
     return {__uint_as_float(a[0] << 16), __uint_as_float(a[0] & 0xffff0000u), __uint_as_float(a[1] << 16),
@@ -544,14 +572,20 @@ template <>
 struct Four<false> {
   typedef float f32x4_4 __attribute__((ext_vector_type(4), aligned(4)));
   f32x4 a;
-  __device__ __forceinline__ void load(const void* p, long long at, int n) {
-    const float* q = (const float*)p + at;
+  __device__ __forceinline__ void load(const void* p, long long row, int c, int H) {
+    const int at = min(c, H - 4);
     a = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (n >= 4) {
-      a = *(const f32x4_4*)q;
-    } else if (n > 0) {
-      const float v[3] = {q[0], q[min(1, n - 1)], q[min(2, n - 1)]};
-      a = f32x4{v[0], n > 1 ? v[1] : 0.f, n > 2 ? v[2] : 0.f, 0.f};
+    if (c - at < 4 && at >= 0) a = *(const f32x4_4*)((const float*)p + row + at);
+  }
+  __device__ __forceinline__ void settle(const void* p, long long row, int c, int H) {
+    if (H < 4) {
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+        if (i < H - c) a[i] = ((const float*)p)[row + c + i];
+    } else {
+      const int s = c - min(c, H - 4);
+      if (s & 1) a = f32x4{a[1], a[2], a[3], 0.f};
+      if (s & 2) a = f32x4{a[2], a[3], 0.f, 0.f};
     }
   }
   __device__ __forceinline__ f32x4 get() const { return a; }
@@ -566,26 +600,34 @@ struct Four<false> {
     }
   }
 };
-__device__ __forceinline__ f32x4 four_weights(const void* p, bool bf16, int c, int n) {
-  if (bf16) {
-    Four<true> f;
-    f.load(p, c, n);
+// Four weights of either type: loaded with others, converted where they are used.
+struct FourWeights {
+  Four<true> b;
+  Four<false> f;
+  __device__ __forceinline__ void load(const void* p, bool bf16, int c, int H) {
+    if (bf16) b.load(p, 0, c, H);
+    else f.load(p, 0, c, H);
+  }
+  __device__ __forceinline__ f32x4 get(const void* p, bool bf16, int c, int H) {
+    if (bf16) {
+      if (H % 4) b.settle(p, 0, c, H);
+      return b.get();
+    }
+    if (H % 4) f.settle(p, 0, c, H);
     return f.get();
   }
-  Four<false> f;
-  f.load(p, c, n);
-  return f.get();
-}
+};
 
 enum { kAfterSum, kGateSum, kBeforeSum, kSums };
-// How many of the columns' sums a launch can take.
-constexpr int sums_of(int U) { return U > 2 ? 2 : 3; }   // (of long rows)
+// How many of the columns' sums a launch for long rows has LDS for, beside a row.
+constexpr int sums_of(int U) { return U > 2 ? 1 : 3; }
 
+// (four waves a SIMD, 128 registers; two where a thread keeps eight columns)
 template <int NT, int U, bool H16, bool Y16, bool Z16, bool kY>
-__global__ void __launch_bounds__(NT) join_grad_kernel(JoinArgs a) {
+__global__ void __launch_bounds__(NT, NT == 1024 || U == 1 ? 4 : 2) join_grad_kernel(JoinArgs a) {
   constexpr bool kLong = NT == 1024;
   __shared__ float lds[3 * NT / 64];
-  __shared__ f32x4 long_sums[kLong ? sums_of(U) : 1][kLong ? U * NT : 1];
+  __shared__ f32x4 long_sums[kLong ? sums_of(U) : 1][kLong ? U * NT : 1], long_d[kLong && kY ? U * NT : 1];
   uint64_t seed = 0, offset = 0;
   if (a.drop) seed = a.rng[0], offset = a.rng[1];
   const bool norm_x = a.before && a.dz, token = kY && a.gate_kind == MOE_GATE_TOKEN,
@@ -594,24 +636,26 @@ __global__ void __launch_bounds__(NT) join_grad_kernel(JoinArgs a) {
   const int place[kSums] = {0, want[0], want[0] + want[1]};   // of each sum that is wanted
   const void* const weights[kSums] = {a.after, a.gate, a.before};
   const bool use[kSums] = {after, channel, norm_x};
-  f32x4 sum[kSums][kLong ? 1 : U] = {}, w[kSums][kLong ? 1 : U] = {};
+  f32x4 sum[kSums][kLong ? 1 : U] = {};
   const int c0 = 4 * (int)threadIdx.x;
-  if (kLong) {
-    for (int k = 0; k < sums_of(U); ++k)
-#pragma unroll
-      for (int u = 0; u < U; ++u) long_sums[k][u * NT + threadIdx.x] = f32x4{0.f, 0.f, 0.f, 0.f};
-  } else {
+  // the weights of four columns: kept, or (long rows) loaded with the columns
+  struct Weights {
+    f32x4 w[kSums];
+  };
+  Weights kept[kLong ? 1 : U];
+  FourWeights raw_w[kSums];
+  auto load_weights = [&](int u, bool first) {   // first: of those that the first pass over a row needs
 #pragma unroll
     for (int k = 0; k < kSums; ++k)
+      if (use[k] && (k == kBeforeSum || !first)) raw_w[k].load(weights[k], a.w16, 4 * NT * u + c0, a.H);
+  };
+  auto get_weights = [&](int u, bool first) {
+    Weights o;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int c = 4 * NT * u + c0;
-        if (use[k]) w[k][u] = four_weights(weights[k], a.w16, c, a.H - c);
-      }
-  }
-  auto weight = [&](int k, int u) {
-    const int c = 4 * NT * u + c0;
-    return kLong ? four_weights(weights[k], a.w16, c, a.H - c) : w[k][kLong ? 0 : u];
+    for (int k = 0; k < kSums; ++k)
+      o.w[k] = use[k] && (k == kBeforeSum || !first) ? raw_w[k].get(weights[k], a.w16, 4 * NT * u + c0, a.H)
+                                                     : f32x4{1.f, 1.f, 1.f, 1.f};
+    return o;
   };
   auto add = [&](int k, int u, f32x4 v) {
     if (!kLong) sum[k][kLong ? 0 : u] += v;
@@ -625,20 +669,35 @@ __global__ void __launch_bounds__(NT) join_grad_kernel(JoinArgs a) {
   } next[kLong ? 1 : U], now[kLong ? 1 : U];
   auto load = [&](Rows& o, long long t, int u) {
     const int c = 4 * NT * u + c0;
-    const long long at = t * a.H + c;
+    const long long row = t * a.H;
     if (norm_x) {
-      o.x.load(a.h, at, a.H - c);
-      o.z.load(a.dz, at, a.H - c);
+      o.x.load(a.h, row, c, a.H);
+      o.z.load(a.dz, row, c, a.H);
     }
-    if (kY) o.y.load(a.y, at, a.H - c);
-    if (a.dx) o.d.load(a.dx, at, a.H - c);
+    if (kY) o.y.load(a.y, row, c, a.H);
+    if (a.dx) o.d.load(a.dx, row, c, a.H);
     if (token) o.gate = element(a.gate, a.w16, t);
   };
   // (a long row's columns come again for each use, by loops that stay loops: unrolled they
   // take more registers than there are)
   constexpr int kUnroll = kLong ? 1 : U;
-  auto columns = [&](long long t, int u) -> const Rows& {
-    if (kLong) load(now[0], t, u);
+  auto settle = [&](Rows& o, long long t, int u) {
+    const int c = 4 * NT * u + c0;
+    const long long row = t * a.H;
+    if (norm_x) {
+      o.x.settle(a.h, row, c, a.H);
+      o.z.settle(a.dz, row, c, a.H);
+    }
+    if (kY) o.y.settle(a.y, row, c, a.H);
+    if (a.dx) o.d.settle(a.dx, row, c, a.H);
+  };
+  auto columns = [&](long long t, int u, bool first) -> const Rows& {
+    if (kLong) {
+      load(now[0], t, u);
+      load_weights(u, first);
+      if (a.H % 4) settle(now[0], t, u);
+      kept[0] = get_weights(u, first);
+    }
     return now[kLong ? 0 : u];
   };
   auto prefetch = [&](long long t) {
@@ -647,16 +706,31 @@ __global__ void __launch_bounds__(NT) join_grad_kernel(JoinArgs a) {
     for (int u = 0; u < (kLong ? 1 : U); ++u) load(next[u], t, u);
   };
   prefetch(blockIdx.x);
+  if (kLong) {
+    for (int k = 0; k < sums_of(U); ++k)
+#pragma unroll
+      for (int u = 0; u < U; ++u) long_sums[k][u * NT + threadIdx.x] = f32x4{0.f, 0.f, 0.f, 0.f};
+  } else {
+#pragma unroll
+    for (int u = 0; u < (kLong ? 1 : U); ++u) {
+      load_weights(u, false);
+      kept[u] = get_weights(u, false);
+    }
+  }
   for (long long t = blockIdx.x; t < a.T; t += gridDim.x) {
 #pragma unroll
-    for (int u = 0; u < (kLong ? 1 : U); ++u) now[u] = next[u];
+    for (int u = 0; u < (kLong ? 1 : U); ++u) {
+      now[u] = next[u];
+      if (!kLong && a.H % 4) settle(now[u], t, u);
+    }
     prefetch(t + gridDim.x);
     float s[3] = {0.f, 0.f, 0.f};   // of x^2, x v, y^2
 #pragma unroll kUnroll
     for (int u = 0; u < U; ++u) {
-      const Rows& row = columns(t, u);
+      const int c = 4 * NT * u + c0;
+      const Rows& row = columns(t, u, true);
       if (norm_x) {
-        const f32x4 x = row.x.get(), v = row.z.get() * weight(kBeforeSum, u);
+        const f32x4 x = row.x.get(), v = row.z.get() * kept[kLong ? 0 : u].w[kBeforeSum];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           s[0] = fmaf(x[i], x[i], s[0]);
@@ -672,47 +746,49 @@ __global__ void __launch_bounds__(NT) join_grad_kernel(JoinArgs a) {
     row_sums<NT>(s, lds);
     const float r = rsqrtf(s[0] / a.H + a.eps), m = r * r * (s[1] / a.H);
     const float q = after ? rsqrtf(s[2] / a.H + a.eps) : 1.f;
-    f32x4 d[U];
+    f32x4 short_d[kLong ? 1 : U];
     float s2[2] = {0.f, 0.f};   // of y v of the norm after the block, and da b
 #pragma unroll kUnroll
     for (int u = 0; u < U; ++u) {
       const int c = 4 * NT * u + c0;
       const long long at = t * a.H + c;
-      const Rows& row = columns(t, u);
-      d[u] = a.dx ? row.d.get() : f32x4{0.f, 0.f, 0.f, 0.f};
+      const Rows& row = columns(t, u, false);
+      f32x4 d = a.dx ? row.d.get() : f32x4{0.f, 0.f, 0.f, 0.f};
       if (norm_x) {
-        const f32x4 x = row.x.get(), z = row.z.get(), v = z * weight(kBeforeSum, u);
+        const f32x4 x = row.x.get(), z = row.z.get(), v = z * kept[kLong ? 0 : u].w[kBeforeSum];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) d[u][i] = fmaf(r, fmaf(-m, x[i], v[i]), d[u][i]);
+        for (int i = 0; i < 4; ++i) d[i] = fmaf(r, fmaf(-m, x[i], v[i]), d[i]);
         add(kBeforeSum, u, z * (x * r));
       }
-      if (a.dh) Four<H16>::put(a.dh, at, a.H - c, d[u]);
-      d[u] *= a.scale;
+      if (a.dh) Four<H16>::put(a.dh, at, a.H - c, d);
+      d *= a.scale;
       if (a.drop) {
         uint32_t word[4];
         philox((uint32_t)(c / 4), (uint32_t)t, offset, seed, word);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) d[u][i] = word[i] >= a.least ? d[u][i] * a.keep : 0.f;
+        for (int i = 0; i < 4; ++i) d[i] = word[i] >= a.least ? d[i] * a.keep : 0.f;
       }
       if (kY) {
         const f32x4 y = row.y.get(), yn = y * q;
-        const f32x4 wa = after ? weight(kAfterSum, u) : f32x4{1.f, 1.f, 1.f, 1.f}, da = d[u], b = yn * wa;
+        const f32x4 wa = kept[kLong ? 0 : u].w[kAfterSum], da = d, b = yn * wa;
         if (channel) {
           add(kGateSum, u, da * b);
-          d[u] *= weight(kGateSum, u);
+          d *= kept[kLong ? 0 : u].w[kGateSum];
         } else if (token) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) s2[1] = fmaf(da[i], b[i], s2[1]);
-          d[u] *= row.gate;
+          d *= row.gate;
         }
         if (after) {
-          add(kAfterSum, u, d[u] * yn);
-          d[u] *= wa;
+          add(kAfterSum, u, d * yn);
+          d *= wa;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s2[0] = fmaf(d[u][i], y[i], s2[0]);
+          for (int i = 0; i < 4; ++i) s2[0] = fmaf(d[i], y[i], s2[0]);
         }
+        if (kLong) long_d[u * NT + threadIdx.x] = d;
+        else short_d[kLong ? 0 : u] = d;
       } else if (a.dy) {
-        Four<Y16>::put(a.dy, at, a.H - c, d[u]);
+        Four<Y16>::put(a.dy, at, a.H - c, d);
       }
     }
     if (!kY) continue;
@@ -726,13 +802,17 @@ __global__ void __launch_bounds__(NT) join_grad_kernel(JoinArgs a) {
 #pragma unroll kUnroll
     for (int u = 0; u < U; ++u) {
       const int c = 4 * NT * u + c0;
+      f32x4 d = kLong ? long_d[u * NT + threadIdx.x] : short_d[kLong ? 0 : u];
       if (after) {
-        if (kLong) now[0].y.load(a.y, t * a.H + c, a.H - c);
+        if (kLong) {
+          now[0].y.load(a.y, t * a.H, c, a.H);
+          if (a.H % 4) now[0].y.settle(a.y, t * a.H, c, a.H);
+        }
         const f32x4 y = now[kLong ? 0 : u].y.get();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) d[u][i] = q * fmaf(-k, y[i], d[u][i]);
+        for (int i = 0; i < 4; ++i) d[i] = q * fmaf(-k, y[i], d[i]);
       }
-      Four<Y16>::put(a.dy, t * a.H + c, a.H - c, d[u]);
+      Four<Y16>::put(a.dy, t * a.H + c, a.H - c, d);
     }
   }
   // the columns' sums: this workgroup's part of each, or the whole where it is the only one
@@ -777,7 +857,7 @@ __global__ void __launch_bounds__(1024) column_sums_kernel(const float* parts, f
 
 // ---- host -------------------------------------------------------------------------
 
-constexpr int kMaxTopk = 64, kMaxExperts = 1024, kMaxWidth = 16384;
+constexpr int kMaxWidth = 16384;
 
 int check_choice(const void* logits, int32_t T, int32_t E, int32_t topk, int32_t type, int32_t score) {
   if (T < 0 || E < 1 || topk < 1 || topk > E || !type_ok(type) || (score != MOE_SOFTMAX && score != MOE_SIGMOID))
@@ -799,6 +879,17 @@ void with_shape(int E, F f) {
   else if (E <= 128) f(Shape<16, 8>());
   else if (E <= 256) f(Shape<16, 16>());
   else if (E <= 512) f(Shape<64, 8>());
+  else f(Shape<64, 16>());
+}
+
+template <class F>
+void with_choice(int E, F f) {
+  if (E <= 16) f(Shape<4, 4>());
+  else if (E <= 32) f(Shape<8, 4>());
+  else if (E <= 64) f(Shape<8, 8>());
+  else if (E <= 128) f(Shape<8, 16>());
+  else if (E <= 256) f(Shape<16, 16>());
+  else if (E <= 512) f(Shape<16, 32>());
   else f(Shape<64, 16>());
 }
 
@@ -857,6 +948,11 @@ void with_grad_row(int H, F f) {
   else if (H <= 8192) f(Shape<1024, 2>());
   else f(Shape<1024, 4>());
 }
+// The threads that a launch of them needs, where each takes `each` columns once.
+template <class S>
+int threads_of(S, int H, int each) {
+  return S::each > 1 ? S::lanes : (H + 64 * each - 1) / (64 * each) * 64;
+}
 // Workgroups of the gradient: enough to fill the card, few enough that their parts are
 // small beside the rows.
 int grad_groups(int T, int H) {
@@ -879,7 +975,7 @@ extern "C" int moe_choose(const void* logits, const float* bias, int32_t* ids, f
       same(bias, ids))
     return MOE_ERR_INVALID_ARG;
   const hipStream_t s = (hipStream_t)stream;
-  with_shape(E, [&](auto shape) {
+  with_choice(E, [&](auto shape) {
     constexpr int L = decltype(shape)::lanes, R = decltype(shape)::each, per = 256 / L;
     in_launches(T, per, [&](long long first, unsigned blocks) {
       if (logits_type == MOE_BF16)
@@ -940,7 +1036,8 @@ extern "C" int moe_join(const void* h, const void* y, const void* after, const v
   const hipStream_t s = (hipStream_t)stream;
   with_row(H, [&](auto shape) {
     constexpr int NT = decltype(shape)::lanes, U = decltype(shape)::each;
-    in_launches(T, 1, [&](long long first, unsigned blocks) { join_kernel<NT, U><<<blocks, NT, 0, s>>>(a, first); });
+    const int threads = threads_of(shape, H, 8);
+    in_launches(T, 1, [&](long long first, unsigned blocks) { join_kernel<NT, U><<<blocks, threads, 0, s>>>(a, first); });
   });
   return done();
 }
@@ -987,9 +1084,10 @@ extern "C" int moe_join_grad(const void* dx, const void* dz, const void* x, cons
     with_grad_row(H, [&](auto shape) {
       constexpr int NT = decltype(shape)::lanes, U = decltype(shape)::each;
       const bool use_y = a.after || a.gate_kind != MOE_GATE_NONE;
+      const int threads = threads_of(shape, H, 4);
 #define MOE_GRAD(H16, Y16, Z16)                                                      \
-  use_y ? join_grad_kernel<NT, U, H16, Y16, Z16, true><<<(unsigned)G, NT, 0, s>>>(a) \
-        : join_grad_kernel<NT, U, H16, Y16, Z16, false><<<(unsigned)G, NT, 0, s>>>(a)
+  use_y ? join_grad_kernel<NT, U, H16, Y16, Z16, true><<<(unsigned)G, threads, 0, s>>>(a) \
+        : join_grad_kernel<NT, U, H16, Y16, Z16, false><<<(unsigned)G, threads, 0, s>>>(a)
       switch (4 * a.h16 + 2 * a.y16 + a.z16) {
         case 0: MOE_GRAD(false, false, false); break;
         case 1: MOE_GRAD(false, false, true); break;
@@ -1004,15 +1102,20 @@ extern "C" int moe_join_grad(const void* dx, const void* dz, const void* x, cons
     });
     return hipGetLastError() == hipSuccess;
   };
-  if (H > 8192 && arrays > 2) {   // LDS holds two of the columns' sums: the third by a launch of its own
+  // LDS holds one of the columns' sums of the longest rows: the others by launches of their own,
+  // before dh, which may be dx, is written
+  float** const sums[3] = {&a.d_after, channel ? &a.d_gate : nullptr, &a.d_before};
+  int left = arrays;
+  for (int k = 2; H > 8192 && k >= 0 && left > 1; --k) {
+    if (!sums[k] || !*sums[k]) continue;
     JoinArgs b = a;
-    b.dx = b.y = b.after = b.gate = nullptr;   // (d_before needs x and dz alone)
     b.dh = b.dy = nullptr;
-    b.d_after = b.d_gate = nullptr;
-    b.gate_kind = MOE_GATE_NONE;
-    b.drop = false;
-    if (a.parts) b.parts = a.parts + 2LL * G * H;
-    a.d_before = nullptr;
+    b.d_after = k == 0 ? a.d_after : nullptr;
+    b.d_gate = k == 1 ? a.d_gate : nullptr;
+    b.d_before = k == 2 ? a.d_before : nullptr;
+    *sums[k] = nullptr;
+    --left;
+    if (a.parts) b.parts = a.parts + (long long)left * G * H;
     if (!launch(b)) return MOE_ERR_HIP;
   }
   if (!launch(a)) return MOE_ERR_HIP;
