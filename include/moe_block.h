@@ -124,8 +124,8 @@ size_t moe_few_scratch_size(int32_t T, int32_t H, int32_t I, int32_t E, int32_t 
  *   scratch     16-byte aligned, moe_few_scratch_size bytes
  * 0 <= T <= MOE_FEW_TOKENS, 1 <= topk <= 64, 1 <= E <= 1024, H % 8 == 0, I % 16 == 0,
  * H, I <= 2^22, 4 H I < 2^31, min(T topk, E) I < 2^26 (else MOE_ERR_INVALID_ARG or MOE_ERR_UNSUPPORTED).  Products in bf16,
- * sums, activation and the weighted sum over experts in fp32; the activation is rounded
- * once to bf16 between the products, out once to its type. */
+ * sums, activation and the weighted sum over experts in fp32; the activation goes into the
+ * second product as two bf16 parts (16 bits of mantissa), out is rounded once to its type. */
 int moe_few_forward(const void* hidden, const void* w1, const void* w2, const int32_t* ids,
                     const float* gates, void* out, int32_t T, int32_t H, int32_t I, int32_t E,
                     int32_t topk, int32_t first_expert, int32_t out_type, void* scratch,

@@ -148,7 +148,8 @@ def layer(x, w1, w2, ids, gates, first=0):
     [E, H, 2I] (gate, then up columns), w2 [E, I, H].  An fp32 sum of n terms in any
     order is off by at most n 2^-24 of their magnitudes (twice that is allowed, since the
     matrix instruction adds in an order and with roundings of its own); the activation's
-    rounding to bf16 adds 2^-8 of it, its fp32 steps 16 2^-24; silu's slope is below 1.1."""
+    two parts of bf16 are within 2^-8 2^-8 of it, its fp32 steps 16 2^-24, and below
+    2^-126 a part may be lost; silu's slope is below 1.1."""
     T, H = x.shape
     E, I = w2.shape[0], w2.shape[1]
     u = 2.0 ** -24
@@ -164,7 +165,7 @@ def layer(x, w1, w2, ids, gates, first=0):
             with np.errstate(all="ignore"):
                 s = g / (1.0 + np.exp(-g))
             a = s * up
-            ta = 1.1 * tp[:I] * (np.abs(up) + tp[I:]) + np.abs(s) * tp[I:] + (16 * u + 2.0 ** -8) * np.abs(a)
+            ta = 1.1 * tp[:I] * (np.abs(up) + tp[I:]) + np.abs(s) * tp[I:] + (16 * u + 2.0 ** -16) * np.abs(a) + 2.0 ** -126
             y = a @ w2[e]
             ty = ta @ np.abs(w2[e]) + 2 * (I + 64) * u * ((np.abs(a) + ta) @ np.abs(w2[e]))
             out[t] += gates[t, j] * y

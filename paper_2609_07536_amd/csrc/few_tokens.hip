@@ -29,7 +29,8 @@ typedef uint32_t u32x4_2 __attribute__((ext_vector_type(4), aligned(2)));
 // What the first launch leaves for the second of a unit (a slot that is the first to name
 // its expert, or an expert where there are more slots than experts): the expert or -1, the
 // tokens that name it and the sum of each one's gates, in slot order.  The activation of
-// token t for it is row T unit + t.
+// token t for it is row T unit + t of `act`, in two parts of bf16 whose sum has 16 bits of
+// mantissa: rounded to one, it would add as much to the layer's error as a bf16 output does.
 struct Hit {
   int32_t e;
   uint32_t tokens;
@@ -43,7 +44,7 @@ struct FewArgs {
   const float* gates;
   void* out;
   Hit* hits;         // [units]
-  __bf16* act;       // [T units][pitch]
+  __bf16* act;       // [T units][2][pitch]
   float* parts;      // [shares][T][H], where the second launch has several shares
   uint32_t* count;   // [tiles of the second launch]: shares that are there
   int T, H, I, E, topk, first, slots, units, pitch;
@@ -94,9 +95,9 @@ struct Bf16Step {
 };
 // A wave's n steps, the loads of two of them under way; a step past the end is loads of
 // nothing and products of zeros, without a branch, so that the waits stay exact.
-template <class Load, class Use>
+template <class Step, class Load, class Use>
 __device__ __forceinline__ void run_steps(int n, Load load, Use use) {
-  Bf16Step b[2];
+  Step b[2];
   load(b[0], 0);
   load(b[1], 1);
   int i = 0;
@@ -185,26 +186,22 @@ __device__ __forceinline__ u32x4 row8(const __bf16* row, int k, int K) {
   }
   return v;
 }
-// 512 elements from k on of the rows (of K, `pitch` apart) of the tokens in the mask to the
-// wave's LDS, zeros past their end.  The rows of other tokens hold anything: they make
-// results of these tokens only, which nobody takes.  kOdd: K is no multiple of 32.
+// 512 elements from k on of a row (of K) to a row of the wave's LDS, zeros past its end.
+// kOdd: K is no multiple of 32, and the row may start at any element.
 template <bool kOdd>
-__device__ __forceinline__ void rows_to_lds(uint8_t* lds, const __bf16* x, int T, int pitch, uint32_t tokens, int k, int K) {
+__device__ __forceinline__ void row_to_lds(uint8_t* lds, i32x4 rsrc, const __bf16* x, int at, int k, int K) {
   const int lane = threadIdx.x & 63;
   k += 8 * lane;
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (what was there has been read)
-  const i32x4 r = buffer_rsrc(x, 2LL * T * pitch);
-  for (uint32_t m = tokens; m; m &= m - 1) {
-    const int t = __builtin_ctz(m);
-    if constexpr (kOdd)
-      *(u32x4*)(lds + t * kStepBytes + 16 * lane) = row8(x + (long long)t * pitch, k, K);
-    else
-      dma16(r, k < K ? 2u * (t * pitch + k) : kOutOfRange, lds_addr(lds + t * kStepBytes));
-  }
+  if constexpr (kOdd)
+    *(u32x4*)(lds + 16 * lane) = row8(x + at, k, K);
+  else
+    dma16(rsrc, k < K ? 2u * (at + k) : kOutOfRange, lds_addr(lds));
 }
-// The four operands of eight of block 4 j + g of the lane's token.
-__device__ __forceinline__ u32x4 row_operand(const uint8_t* lds, int t, int j, int q) {
-  return *(const u32x4*)(lds + t * kStepBytes + (4 * j + (int)((threadIdx.x & 63) >> 4)) * 2 * kBlock + 16 * q);
+// Before a wave's rows in LDS are written again: what was there has been read.
+__device__ __forceinline__ void rows_read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+// The four operands of eight of block 4 j + g of the lane's row.
+__device__ __forceinline__ u32x4 row_operand(const uint8_t* lds, int row, int j, int q) {
+  return *(const u32x4*)(lds + row * kStepBytes + (4 * j + (int)((threadIdx.x & 63) >> 4)) * 2 * kBlock + 16 * q);
 }
 
 // ---- the first launch ------------------------------------------------------------------
@@ -270,8 +267,7 @@ __device__ __forceinline__ void put_column(float (*lds)[16][COLS], int n, f32x4 
   for (int i = 0; i < 4; ++i) lds[threadIdx.x >> 6][4 * (lane >> 4) + i][n] = v[i];
 }
 
-// silu(gate) * up of the waves' sums, in fp32, rounded once: the second launch's matrix
-// instructions take bf16.
+// silu(gate) * up of the waves' sums, in fp32.
 template <int W, int COLS>
 __device__ __forceinline__ float swiglu(const float (*lds)[16][COLS], int t, int g, int u) {
   float x = 0.f, y = 0.f;
@@ -281,6 +277,15 @@ __device__ __forceinline__ float swiglu(const float (*lds)[16][COLS], int t, int
     y += lds[w][t][u];
   }
   return x / (1.f + expf(-x)) * y;
+}
+
+// An element of a token's activation, in its two parts.
+__device__ __forceinline__ void put_act(const FewArgs& a, int unit, int t, int o, float v) {
+  const __bf16 hi = (__bf16)v;
+  const float rest = v - (float)hi;
+  __bf16* p = a.act + ((long long)a.T * unit + t) * 2 * a.pitch + o;
+  p[0] = hi;
+  p[a.pitch] = (__bf16)(fabsf(rest) < __builtin_inff() ? rest : 0.f);   // (of an infinity there is no rest)
 }
 
 // 64 packed columns (32 outputs), the waves taking every W-th 32 of K.
@@ -299,7 +304,7 @@ __global__ void __launch_bounds__(64 * W) few_up_kernel(FewArgs a) {
   const uint32_t pitch = 2 * N;
   f32x4 acc[4] = {};
   const int steps = (a.H + 31) / 32;
-  run_steps(
+  run_steps<Bf16Step>(
       (steps - wave + W - 1) / W,
       [&](Bf16Step& b, int i) {
         const int k = (wave + i * W) * 32 + g * 8;
@@ -316,7 +321,7 @@ __global__ void __launch_bounds__(64 * W) few_up_kernel(FewArgs a) {
   for (int i = threadIdx.x; i < 16 * kCols / 2; i += 64 * W) {
     const int t = i / (kCols / 2), c = i % (kCols / 2), at = c / 16 * 32 + c % 16, o = tile * (kCols / 2) + c;
     if (((tokens >> t) & 1) && o < a.I)
-      a.act[((long long)a.T * unit + t) * a.pitch + o] = (__bf16)swiglu<W>(lds, t, at, at + 16);
+      put_act(a, unit, t, o, swiglu<W>(lds, t, at, at + 16));
   }
   if (tile == 0) write_hit(a, unit, e, tokens);
 }
@@ -339,7 +344,13 @@ __global__ void __launch_bounds__(64 * W) few_up_mx4_kernel(FewArgs a) {
   const int token = min(n, R - 1);
   for (int kb0 = wave * kStepBlocks; kb0 < KB; kb0 += W * kStepBlocks) {
     Mx4Step<2 * G> b;
-    rows_to_lds<kOdd>(rows[wave], a.x, a.T, a.H, tokens, kb0 * kBlock, a.H);
+    // (rows of tokens that do not name the expert hold anything: they make results that nobody takes)
+    rows_read();
+    const i32x4 rsrc = buffer_rsrc(a.x, 2LL * a.T * a.H);
+    for (uint32_t m = tokens; m; m &= m - 1) {
+      const int t = __builtin_ctz(m);
+      row_to_lds<kOdd>(rows[wave] + t * kStepBytes, rsrc, a.x, t * a.H, kb0 * kBlock, a.H);
+    }
 #pragma unroll
     for (int m = 0; m < 2 * G; ++m) {
       const int c = col + m / 2 * 16;
@@ -365,7 +376,7 @@ __global__ void __launch_bounds__(64 * W) few_up_mx4_kernel(FewArgs a) {
   for (int i = threadIdx.x; i < 256 * G; i += 64 * W) {
     const int t = i / (16 * G), c = i % (16 * G), o = tile * 16 * G + c, at = c / 16 * 32 + c % 16;
     if (((tokens >> t) & 1) && o < a.pitch)
-      a.act[((long long)a.T * unit + t) * a.pitch + o] = (__bf16)(o < a.I ? swiglu<W>(lds, t, at, at + 16) : 0.f);
+      put_act(a, unit, t, o, o < a.I ? swiglu<W>(lds, t, at, at + 16) : 0.f);
   }
   if (tile == 0) write_hit(a, unit, e, tokens);
 }
@@ -419,25 +430,6 @@ struct Part {
   }
 };
 
-// The gates and tokens of a hit, for the four rows of the lane's results.
-struct Gates {
-  f32x4 gate;
-  uint32_t tokens;
-  __device__ __forceinline__ void load(const FewArgs& a, int2 hit) {
-    tokens = (uint32_t)hit.y >> (4 * ((threadIdx.x & 63) >> 4));
-    const float* p = a.hits[(uint32_t)hit.y >> 16].gate + 4 * ((threadIdx.x & 63) >> 4);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) gate[i] = p[i];
-  }
-  __device__ __forceinline__ void add(f32x4& sum, f32x4& acc) const {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      sum[i] = (tokens >> i) & 1 ? fmaf(gate[i], acc[i], sum[i]) : sum[i];
-      acc[i] = 0.f;
-    }
-  }
-};
-
 __device__ __forceinline__ void put_out(const FewArgs& a, int t, int o, float v) {
   if (a.out16)
     ((__bf16*)a.out)[(long long)t * a.H + o] = (__bf16)v;
@@ -487,22 +479,33 @@ __device__ __forceinline__ void join_sums(const FewArgs& a, const float (*lds)[1
   }
 }
 
-template <int W>
+// Up to eight tokens: rows 0 to 7 of the matrix instruction are one part of their
+// activations, rows 8 to 15 the other; more tokens (kMany): an instruction for each part.
+template <int W, bool kMany>
 __global__ void __launch_bounds__(64 * W) few_down_kernel(FewArgs a) {
   __shared__ float lds[W][16][kCols];
   __shared__ int2 hits[kMaxExperts];
+  struct Step : Bf16Step {
+    u32x4 rest;
+  };
   const int share = blockIdx.x / a.out_tiles, tile = blockIdx.x - share * a.out_tiles;
   const int wave = threadIdx.x >> 6, n = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
   const int col = tile * kCols + 4 * n, steps = (a.I + 31) / 32;
+  const int token = kMany ? n : n & 7, part = kMany ? 0 : n >> 3, row0 = kMany ? 4 * g : 4 * (g & 1);
   const Part p = Part::of<W>(list_hits<W>(a, hits), steps, share, a.shares, wave);
-  f32x4 acc[4] = {}, sum[4] = {};
-  Gates gates;
+  f32x4 acc[4] = {}, sum[4] = {}, gate = {};
+  uint32_t named = 0;   // the tokens of the four rows that name the expert
+  auto load_gates = [&](int2 h) {
+    named = (uint32_t)h.y >> row0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) gate[i] = a.hits[(uint32_t)h.y >> 16].gate[row0 + i];
+  };
   int load_u = p.u, load_s = p.s, u = p.u, s = p.s;   // the places of the next load and the next products
   if (p.s0 < p.s1) {
-    gates.load(a, hits[u]);
-    run_steps(
+    load_gates(hits[u]);
+    run_steps<Step>(
         p.s1 - p.s0,
-        [&](Bf16Step& b, int i) {
+        [&](Step& b, int i) {
           const bool live = p.s0 + i < p.s1;
           const int2 h = hits[live ? load_u : p.u];
           const int e = __builtin_amdgcn_readfirstlane(h.x);
@@ -511,69 +514,118 @@ __global__ void __launch_bounds__(64 * W) few_down_kernel(FewArgs a) {
           const int k = load_s * 32 + g * 8;
           const bool in = live && k < a.I;
           b.load(buffer(a.w2 + e * bytes, bytes), in && col < a.H ? (uint32_t)(k * a.H + col) * 2 : kOutOfRange, 2 * a.H);
-          b.x = load16(buffer(a.act + (long long)a.T * (tokens >> 16) * a.pitch, 2LL * a.T * a.pitch),
-                       in && ((tokens >> n) & 1) ? 2u * (n * a.pitch + k) : kOutOfRange);
+          const Buffer x = buffer(a.act + (long long)a.T * (tokens >> 16) * 2 * a.pitch, 4LL * a.T * a.pitch);
+          const uint32_t at = in && ((tokens >> token) & 1) ? 2u * ((2 * token + part) * a.pitch + k) : kOutOfRange;
+          b.x = load16(x, at);
+          if (kMany) b.rest = load16(x, at + 2 * a.pitch);
           if (++load_s == steps) load_s = 0, ++load_u;
         },
-        [&](const Bf16Step& b, int i) {
+        [&](const Step& b, int i) {
           const int at = p.s0 + i;
 #pragma unroll
-          for (int c = 0; c < 4; ++c) acc[c] = mfma(b.x, b.column(c), acc[c]);
+          for (int c = 0; c < 4; ++c) {
+            const u32x4 w = b.column(c);
+            acc[c] = mfma(b.x, w, acc[c]);
+            if (kMany) acc[c] = mfma(b.rest, w, acc[c]);
+          }
           if (at < p.s1 && (s + 1 == steps || at + 1 == p.s1)) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) gates.add(sum[c], acc[c]);
-            if (at + 1 < p.s1) gates.load(a, hits[u + 1]);
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                sum[c][j] = (named >> j) & 1 ? fmaf(gate[j], acc[c][j], sum[c][j]) : sum[c][j];
+                acc[c][j] = 0.f;
+              }
+            if (at + 1 < p.s1) load_gates(hits[u + 1]);
           }
           if (++s == steps) s = 0, ++u;
         });
   }
 #pragma unroll
-  for (int c = 0; c < 4; ++c) put_column(lds, 4 * n + c, sum[c]);
+  for (int c = 0; c < 4; ++c) {
+    if (!kMany) {   // the other part's sums are 32 lanes away
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[c][i] += __shfl_xor(sum[c][i], 32);
+    }
+    if (kMany || g < 2) put_column(lds, 4 * n + c, sum[c]);
+  }
   join_sums<W>(a, lds, share, tile);
 }
 
-// Weights in mx4: 16 columns, a wave's step as in the first launch.
-template <int R, int W>
+// Weights in mx4: 16 columns, a wave's step as in the first launch.  R tokens (up to eight)
+// at a time, rows 0 to 7 of the matrix instruction one part of their activations and rows 8
+// to 15 the other: the tokens that name the expert, one after the other, so that more than R
+// of them, which take another pass over the codes that are there, are rare.
+template <int R, int W, int kPasses>
 __global__ void __launch_bounds__(64 * W) few_down_mx4_kernel(FewArgs a) {
   __shared__ float lds[W][16][16];
   __shared__ int2 hits[kMaxExperts];
-  __shared__ __attribute__((aligned(16))) uint8_t rows[W][R * kStepBytes];
+  __shared__ __attribute__((aligned(16))) uint8_t rows[W][2 * R * kStepBytes];
   const int share = blockIdx.x / a.out_tiles, tile = blockIdx.x - share * a.out_tiles;
-  const int wave = threadIdx.x >> 6, n = threadIdx.x & 15;
+  const int wave = threadIdx.x >> 6, n = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
   const int KB = a.pitch / kBlock, KS = (KB + 3) / 4 * 4, col = tile * 16 + n;
   const int steps = (KB + kStepBlocks - 1) / kStepBlocks;
+  const int row = min(n & 7, R - 1) + (n >> 3) * R;   // of LDS, of this lane's operands
   const long long codes = 16LL * a.H * KB, scales = (long long)a.H * KS;
   const Part p = Part::of<W>(list_hits<W>(a, hits), steps, share, a.shares, wave);
-  f32x4 acc = {}, sum = {};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) lds[wave][4 * g + i][n] = 0.f;
+  f32x4 acc[kPasses] = {};
   bool bad = false;
   int u = p.u, s = p.s;
   for (int at = p.s0; at < p.s1; ++at) {
     const int2 h = hits[u];
     const int e = __builtin_amdgcn_readfirstlane(h.x), kb0 = s * kStepBlocks;
-    const uint32_t tokens = __builtin_amdgcn_readfirstlane(h.y);
+    const uint32_t tokens = __builtin_amdgcn_readfirstlane(h.y), unit = tokens >> 16;
+    const __bf16* x = a.act + (long long)a.T * unit * 2 * a.pitch;
+    const i32x4 rsrc = buffer_rsrc(x, 4LL * a.T * a.pitch);
     Mx4Step<1> b;
-    Gates gates;
-    const bool ends = s + 1 == steps || at + 1 == p.s1;
-    rows_to_lds<false>(rows[wave], a.act + (long long)a.T * (tokens >> 16) * a.pitch, a.T, a.pitch, tokens & 0xffff,
-                       kb0 * kBlock, a.pitch);
     b.load(0, buffer(a.w2 + e * codes, codes), buffer(a.w2_scales + e * scales, scales), col, kb0, KB, KS, col < a.H);
-    if (ends) gates.load(a, h);
-    waitcnt_vm<0>();
-    asm volatile("" ::: "memory");
-    b.align(kb0, KS);
+    const bool ends = s + 1 == steps || at + 1 == p.s1;
+    uint32_t m = tokens & 0xffff;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int pass = 0; pass < kPasses; ++pass) {
+      if (m == 0) break;
+      rows_read();
+      // the pass's tokens, each also in the lanes that have its results (rows 4 g + i, g < 2)
+      int token[4] = {0, 0, 0, 0};
+      uint32_t there = 0;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) acc = mfma(row_operand(rows[wave], min(n, R - 1), j, q), b.eight(0, j, q), acc);
-    bad |= b.bad(0, kb0, KB);
-    if (ends) {
-      acc = with_nan(acc, bad);
-      gates.add(sum, acc);
-      bad = false;
+      for (int r = 0; r < R; ++r) {
+        if (m == 0) break;
+        const int t = __builtin_ctz(m);
+        m &= m - 1;
+        row_to_lds<false>(rows[wave] + r * kStepBytes, rsrc, x, 2 * t * a.pitch, kb0 * kBlock, a.pitch);
+        row_to_lds<false>(rows[wave] + (R + r) * kStepBytes, rsrc, x, (2 * t + 1) * a.pitch, kb0 * kBlock, a.pitch);
+        token[r % 4] = r / 4 == (g & 1) ? t : token[r % 4];
+        there |= 1u << r;
+      }
+      float gate[4];
+      if (ends) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) gate[i] = a.hits[unit].gate[token[i]];
+      }
+      waitcnt_vm<0>();
+      asm volatile("" ::: "memory");
+      if (pass == 0) b.align(kb0, KS);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) acc[pass] = mfma(row_operand(rows[wave], row, j, q), b.eight(0, j, q), acc[pass]);
+      if (pass == 0) bad |= b.bad(0, kb0, KB);
+      if (ends) {
+        const f32x4 v = with_nan(acc[pass], bad);
+        acc[pass] = f32x4{};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float both = v[i] + __shfl_xor(v[i], 32);   // the other part's
+          if (g < 2 && ((there >> (4 * g + i)) & 1)) lds[wave][token[i]][n] = fmaf(gate[i], both, lds[wave][token[i]][n]);
+        }
+      }
     }
+    if (ends) bad = false;
     if (++s == steps) s = 0, ++u;
   }
-  put_column(lds, n, sum);
   join_sums<W>(a, lds, share, tile);
 }
 
@@ -610,7 +662,7 @@ Layout layout_of(int T, int H, int I, int E, int topk) {
   const size_t units = T * topk < E ? T * topk : E;
   Layout l;
   l.act = up16(units * sizeof(Hit));
-  l.count = l.act + up16(units * T * act_pitch(I) * sizeof(__bf16));
+  l.count = l.act + up16(units * T * 2 * act_pitch(I) * sizeof(__bf16));
   l.parts = l.count + up16((size_t)(H + 15) / 16 * sizeof(uint32_t));
   size_t parts = 0;
   for (const bool mx4 : {false, true}) {
@@ -675,10 +727,10 @@ int few(bool mx4, const void* hidden, const void* w1, const void* w1_scales, con
     up<<<(unsigned)(units * a.tiles), 64 * waves, 0, s>>>(a);
   }
   if (hipGetLastError() != hipSuccess) return MOE_ERR_HIP;
-  auto down = !mx4     ? few_down_kernel<8>
-              : T <= 4 ? few_down_mx4_kernel<4, 16>
-              : T <= 8 ? few_down_mx4_kernel<8, 8>
-                       : few_down_mx4_kernel<16, 8>;
+  auto down = !mx4     ? (T <= 8 ? few_down_kernel<8, false> : few_down_kernel<8, true>)
+              : T <= 4 ? few_down_mx4_kernel<4, 16, 1>
+              : T <= 8 ? few_down_mx4_kernel<8, 8, 1>
+                       : few_down_mx4_kernel<8, 8, 2>;
   down<<<(unsigned)(d.tiles * d.shares), 64 * d.waves, 0, s>>>(a);
   return done();
 }
