@@ -33,7 +33,8 @@
  *           slot of a token names add nothing to it (not 0 times something).
  *
  * Sums and statistics are fp32, in an order that sizes alone decide: results do not
- * vary from run to run.
+ * vary from run to run.  Calls that may run at the same time (on two streams, or in two
+ * graphs) need scratch of their own.
  */
 #ifndef MOE_BLOCK_H
 #define MOE_BLOCK_H
@@ -123,9 +124,11 @@ size_t moe_few_scratch_size(int32_t T, int32_t H, int32_t I, int32_t E, int32_t 
  *   out         device [T, H] of out_type, fully written
  *   scratch     16-byte aligned, moe_few_scratch_size bytes
  * 0 <= T <= MOE_FEW_TOKENS, 1 <= topk <= 64, 1 <= E <= 1024, H % 8 == 0, I % 16 == 0,
- * H, I <= 2^22, 4 H I < 2^31, min(T topk, E) I < 2^26 (else MOE_ERR_INVALID_ARG or MOE_ERR_UNSUPPORTED).  Products in bf16,
- * sums, activation and the weighted sum over experts in fp32; the activation goes into the
- * second product as two bf16 parts (16 bits of mantissa), out is rounded once to its type. */
+ * H, I <= 2^22, 4 H I < 2^31, min(T topk, E) I < 2^26 (else MOE_ERR_INVALID_ARG or
+ * MOE_ERR_UNSUPPORTED).  Products in bf16, sums, activation and the weighted sum over experts in fp32; the activation goes into the
+ * second product as two bf16 parts (16 bits of mantissa; one beyond bf16's range counts as
+ * infinite), out is rounded once to its type.  An infinite weight of w2 makes NaN of the
+ * sums that it enters, whichever sign they would have. */
 int moe_few_forward(const void* hidden, const void* w1, const void* w2, const int32_t* ids,
                     const float* gates, void* out, int32_t T, int32_t H, int32_t I, int32_t E,
                     int32_t topk, int32_t first_expert, int32_t out_type, void* scratch,
@@ -133,8 +136,9 @@ int moe_few_forward(const void* hidden, const void* w1, const void* w2, const in
 
 /* The same with weights in mx4 (w1 [E, 2 I, H]: an expert's I gate rows, then its I up
  * rows; w2 [E, H, I]) and activations in bf16: what a weight stands for is exact in the
- * products.  Limits as above, but any H and I whose codes are below 2 GiB an expert.  A value below 2^-126
- * may count as zero.  NaN blocks make the sums that they enter NaN. */
+ * products.  Limits as above, but any H and I whose codes are below 2 GiB an expert.  A
+ * value below 2^-126 may count as zero.  NaN blocks make the sums that they enter NaN; pad
+ * bytes of scales are not used. */
 int moe_few_forward_mx4(const void* hidden, const void* w1_codes, const void* w1_scales,
                         const void* w2_codes, const void* w2_scales, const int32_t* ids,
                         const float* gates, void* out, int32_t T, int32_t H, int32_t I, int32_t E,

@@ -141,6 +141,8 @@ def join(h, y=None, after=None, gate=None, scale: float = 1.0, drop: float = 0.0
     """block.join with the gradients of h, y, after, gate and before.  h None: nothing to
     add to.  y None: the norm of h alone."""
     if y is None:
+        if h is None or before is None or after is not None or gate is not None or drop:
+            raise TypeError("without y: expected h and `before`, and neither a norm after the block, a gate nor dropout")
         # (the stream itself goes on as it is: its gradient meets the norm's at h)
         return K.Joined(h, _Norm.apply(h, before, eps, dtype))
     return K.Joined(*_Join.apply(h, y, after, gate, before, scale, drop, rng, eps, dtype))

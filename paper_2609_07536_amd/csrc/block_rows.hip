@@ -77,12 +77,11 @@ __device__ __forceinline__ void load_logits(const T* p, int E, int l, float (&v)
 
 __device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
 
-// A float's bits in an order that integers compare by (NaN aside), and back.
+// A float's bits in an order that integers compare by (NaN aside).
 __device__ __forceinline__ int ordered(float v) {
   const int b = __float_as_int(v);
   return b ^ ((b >> 31) & 0x7fffffff);
 }
-__device__ __forceinline__ float unordered(int k) { return __int_as_float(k ^ ((k >> 31) & 0x7fffffff)); }
 
 // Bound by the instructions of the rounds: for each logit of a lane two comparisons and two
 // selections (16384 tokens, 8 of 256 experts by sixteen lanes a token: 10.8 us, of which
@@ -727,7 +726,6 @@ __global__ void __launch_bounds__(NT, NT == 1024 || U == 1 ? 4 : 2) join_grad_ke
     float s[3] = {0.f, 0.f, 0.f};   // of x^2, x v, y^2
 #pragma unroll kUnroll
     for (int u = 0; u < U; ++u) {
-      const int c = 4 * NT * u + c0;
       const Rows& row = columns(t, u, true);
       if (norm_x) {
         const f32x4 x = row.x.get(), v = row.z.get() * kept[kLong ? 0 : u].w[kBeforeSum];
@@ -907,8 +905,9 @@ int check_join(const JoinArgs& a, int32_t T, int32_t H, int32_t h_type, int32_t 
       gate_kind < MOE_GATE_NONE || gate_kind > MOE_GATE_CHANNEL || !(drop >= 0.0 && drop < 1.0))
     return MOE_ERR_INVALID_ARG;
   if (H > kMaxWidth) return MOE_ERR_UNSUPPORTED;
+  if (gate_kind == MOE_GATE_CHANNEL && !a.gate) return MOE_ERR_INVALID_ARG;
   if (T > 0) {   // (tensors of no rows may have no address)
-    if ((gate_kind != MOE_GATE_NONE && !a.gate) || (drop > 0.0 && !a.rng)) return MOE_ERR_INVALID_ARG;
+    if ((gate_kind == MOE_GATE_TOKEN && !a.gate) || (drop > 0.0 && !a.rng)) return MOE_ERR_INVALID_ARG;
     if (!a.y && (a.after || gate_kind != MOE_GATE_NONE || drop > 0.0)) return MOE_ERR_INVALID_ARG;
   }
   const size_t h = type_size(h_type), y = type_size(y_type), z = type_size(z_type), w = type_size(w_type);

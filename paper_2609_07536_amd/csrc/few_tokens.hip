@@ -137,11 +137,19 @@ struct Mx4Step {
         scale[n][j] = __builtin_amdgcn_raw_buffer_load_b32(s, in && 4 * j < KS ? r * KS + 4 * j : kOutOfRange, 0, 0);
     }
   }
-  // brings the scales of blocks kb0 + 4 j .. into scale[n][j]
-  __device__ __forceinline__ void align(int kb0, int KS) {
+  // brings the scales of blocks kb0 + 4 j .. into scale[n][j], zeros for blocks past the row's
+  // (their bytes in memory are anything, and 255 would make NaN of codes of zeros)
+  __device__ __forceinline__ void align(int kb0, int KB, int KS) {
     for (int past = kb0 + kStepBlocks - KS; KS >= kStepBlocks && past > 0; past -= 4)
 #pragma unroll
       for (int n = 0; n < N; ++n) scale[n] = u32x4{scale[n][1], scale[n][2], scale[n][3], 0};
+    if (kb0 + kStepBlocks > KB) {   // (uniform)
+      const int first = kb0 + (int)((threadIdx.x & 63) >> 4);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int n = 0; n < N; ++n) scale[n][j] = first + 4 * j < KB ? scale[n][j] : 0;
+    }
   }
   __device__ __forceinline__ uint32_t byte(int n, int j) const {
     return (scale[n][j] >> (((threadIdx.x & 63) >> 4) * 8)) & 255;
@@ -157,10 +165,10 @@ struct Mx4Step {
             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3))};
   }
   // whether one of the lane's blocks is NaN
-  __device__ __forceinline__ bool bad(int n, int kb0, int KB) const {
+  __device__ __forceinline__ bool bad(int n) const {
     bool r = false;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) r |= byte(n, j) == 255 && kb0 + 4 * j + (int)((threadIdx.x & 63) >> 4) < KB;
+    for (int j = 0; j < 4; ++j) r |= byte(n, j) == 255;
     return r;
   }
 };
@@ -358,7 +366,7 @@ __global__ void __launch_bounds__(64 * W) few_up_mx4_kernel(FewArgs a) {
     }
     waitcnt_vm<0>();
     asm volatile("" ::: "memory");
-    b.align(kb0, KS);
+    b.align(kb0, KB, KS);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -368,7 +376,7 @@ __global__ void __launch_bounds__(64 * W) few_up_mx4_kernel(FewArgs a) {
         for (int m = 0; m < 2 * G; ++m) acc[m] = mfma(v, b.eight(m, j, q), acc[m]);
       }
 #pragma unroll
-    for (int m = 0; m < 2 * G; ++m) bad[m] |= b.bad(m, kb0, KB);
+    for (int m = 0; m < 2 * G; ++m) bad[m] |= b.bad(m);
   }
 #pragma unroll
   for (int m = 0; m < 2 * G; ++m) put_column(lds, 16 * m + n, with_nan(acc[m], bad[m]));
@@ -607,12 +615,12 @@ __global__ void __launch_bounds__(64 * W) few_down_mx4_kernel(FewArgs a) {
       }
       waitcnt_vm<0>();
       asm volatile("" ::: "memory");
-      if (pass == 0) b.align(kb0, KS);
+      if (pass == 0) b.align(kb0, KB, KS);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int q = 0; q < 4; ++q) acc[pass] = mfma(row_operand(rows[wave], row, j, q), b.eight(0, j, q), acc[pass]);
-      if (pass == 0) bad |= b.bad(0, kb0, KB);
+      if (pass == 0) bad |= b.bad(0);
       if (ends) {
         const f32x4 v = with_nan(acc[pass], bad);
         acc[pass] = f32x4{};

@@ -207,3 +207,19 @@ def test_join_gradient_against_differences(kind, norms):
             d = np.zeros_like(v)
             d[i] = 1e-5
             assert abs((f(**{name: v + d}) - f(**{name: v - d})) / 2e-5 - got[name][0][i]) < 1e-7, (name, i)
+
+
+def test_a_gate_of_channels_is_needed_without_tokens_too():
+    """Its H elements are read for the sums over no rows."""
+    assert _grad(T=0, gate=None) == _join(T=0, gate=None, kind=2) == B.MOE_ERR_INVALID_ARG
+    assert _join(T=0, gate=None) == B.MOE_OK
+
+
+def test_a_differentiable_norm_alone_refuses_what_it_would_leave_out():
+    from paper_2609_07536_amd import autograd as A
+    x, w = torch.zeros(4, 8), torch.ones(8)
+    for bad in (dict(before=w, gate=torch.ones(1, 8)), dict(before=w, after=w), dict(before=w, drop=0.5), dict()):
+        with pytest.raises(TypeError):
+            A.join(x, **bad)
+    with pytest.raises(TypeError):
+        A.join(None, before=w)

@@ -1,0 +1,159 @@
+"""GPU: choose, join, their gradients and layer_few at the ends of their ranges:
+tensors past 2^31 elements and past 2^20 rows, every sum of long rows at once, every
+type with every other, bytes of scales that stand for nothing, two streams at once.
+What lies past 2^31 elements is compared with the same call on a copy of the last rows
+(which has to give the same bits; the oracle pins the small calls), random numbers
+with the oracle's."""
+import itertools
+
+import numpy as np
+import pytest
+
+from oracle import block as ob
+from test_gpu_block import test_join_grad as check_join_grad
+from test_gpu_few import _case, _check, _mx4, _pack, _run
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def _free_after():
+    yield
+    import torch
+    torch.cuda.empty_cache()
+
+
+def _tail(t, n=3000):
+    return t[-n:].clone()
+
+
+def test_choose_past_32_bits(gpu_lib):
+    import torch
+
+    from paper_2609_07536_amd import block as K
+    T, E = 2 ** 28 + 37, 8
+    logits = torch.empty(T, E, dtype=torch.bfloat16, device="cuda").normal_()
+    got = K.choose(logits, 1, score="sigmoid", renormalize=False)
+    want = K.choose(_tail(logits), 1, score="sigmoid", renormalize=False)
+    for a, b in zip(got, want):
+        assert torch.equal(_tail(a), b)
+    middle = slice(2 ** 26 - 50, 2 ** 26 + 50)      # (where a second launch begins)
+    assert torch.equal(got.expert_ids[middle, 0].long(), logits[middle].float().max(1).indices)
+    d = K.choose_grad(got.gates, logits, got.expert_ids, score="sigmoid", renormalize=False)
+    ref = K.choose_grad(_tail(got.gates), _tail(logits), _tail(got.expert_ids), score="sigmoid", renormalize=False)
+    assert torch.equal(_tail(d), ref)
+
+
+@pytest.mark.parametrize("T,H", [(2 ** 28 + 37, 8), (2 ** 17 + 5, 16384)])
+def test_join_past_32_bits(gpu_lib, T, H):
+    import torch
+
+    from paper_2609_07536_amd import block as K
+    h = torch.empty(T, H, dtype=torch.bfloat16, device="cuda").normal_()
+    y = torch.empty(T, H, dtype=torch.bfloat16, device="cuda").normal_()
+    gate, w = torch.rand(T, 1, device="cuda"), torch.rand(H, device="cuda")
+    n = 3000 if H < 100 else 5
+    want = K.join(_tail(h, n), _tail(y, n), after=w, gate=_tail(gate, n), before=w)
+    r = K.join(h, y, after=w, gate=gate, before=w, out=K.Joined(h, torch.empty_like(h)))
+    assert torch.equal(_tail(r.h, n), want.h) and torch.equal(_tail(r.z, n), want.z)
+    # the gradients of r.z: of tokens' gates, and of y into the memory of h
+    kw = dict(after=w, before=w)
+    want = K.join_grad(_tail(r.z, n), None, None, _tail(y, n), gate=_tail(gate, n), **kw)
+    out = K.JoinGrads(None, h, None, torch.empty(T, 1, device="cuda"), None)
+    K.join_grad(r.z, None, None, y, gate=gate, out=out, **kw)
+    assert torch.equal(_tail(out.gate, n), want.gate) and torch.equal(_tail(out.y, n), want.y)
+
+
+def test_random_numbers_of_late_rows(gpu_lib):
+    import torch
+
+    from paper_2609_07536_amd import block as K
+    T, H, p = 2 ** 28 + 37, 8, 0.4
+    rng = torch.tensor([12345, -7], device="cuda")
+    x = K.join(None, torch.ones(T, H, dtype=torch.bfloat16, device="cuda"), drop=p, rng=rng).h
+    for t in (0, 1, 2 ** 20 - 1, 2 ** 20, 2 ** 27 + 3, T - 1):
+        words = [w for c in range(H // 4) for w in ob.philox((c, t, (-7) & 0xffffffff, 0xffffffff), (12345, 0))]
+        assert (x[t] != 0).tolist() == [w >= int(p * 2 ** 32) for w in words], t
+
+
+@pytest.mark.parametrize("mx4", [False, True])
+def test_few_with_weights_past_32_bits(gpu_lib, mx4):
+    """The last 32 experts of many, and a copy of them alone."""
+    import torch
+
+    from paper_2609_07536_amd import block as K
+    from paper_2609_07536_amd import experts as X
+    T, k, n = 5, 4, 32
+    H, I, E = (4096, 1100, 1000) if mx4 else (2048, 704, 800)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+
+    def codes(rows, K_):
+        blocks = (K_ + 31) // 32
+        c = torch.randint(0, 256, (E, rows, blocks, 16), dtype=torch.uint8, device="cuda", generator=gen)
+        s = torch.randint(115, 122, (E, rows, (blocks + 3) // 4 * 4), dtype=torch.uint8, device="cuda", generator=gen)
+        if K_ % 32:   # (a last block's elements past the row are zeros)
+            last = torch.arange(16, device="cuda") < K_ % 32 // 2
+            c[..., -1, :] *= last
+        return X.MX4(c.view(*X._mx4_shapes((E, rows), K_)[0]), s.view(*X._mx4_shapes((E, rows), K_)[1]), K_)
+    if mx4:
+        w1, w2 = codes(2 * I, H), codes(H, I)
+        assert w1.codes.numel() > 2 ** 31 and w2.codes.numel() > 2 ** 31
+        few = [X.MX4(w.codes[-n:].clone(), w.scales[-n:].clone(), w.K) for w in (w1, w2)]
+    else:
+        w1 = torch.empty(E, H, 2 * I, dtype=torch.bfloat16, device="cuda").normal_(0, H ** -0.5, generator=gen)
+        w2 = torch.empty(E, I, H, dtype=torch.bfloat16, device="cuda").normal_(0, I ** -0.5, generator=gen)
+        assert w1.numel() > 2 ** 31
+        few = [w[-n:].clone() for w in (w1, w2)]
+    x = torch.randn(T, H, device="cuda", generator=gen).bfloat16()
+    ids = E - 1 - torch.arange(T * k, device="cuda", dtype=torch.int32).view(T, k)
+    gates = torch.rand(T, k, device="cuda", generator=gen)
+    got = K.layer_few(x, w1, w2, ids, gates)
+    want = K.layer_few(x, *few, ids, gates, first_expert=E - n)
+    assert torch.equal(got, want) and bool(got.isfinite().all()) and bool(got.any())
+
+
+@pytest.mark.parametrize("T,H", [(1, 9000), (6, 8193), (5, 16384), (7, 8190), (9, 4100), (600, 520)])
+@pytest.mark.parametrize("h,y,z,w", [("bfloat16", "float32", "bfloat16", "float32"), ("float32", "bfloat16", "float32", "bfloat16")])
+def test_every_sum_over_rows_at_once(gpu_lib, T, H, h, y, z, w):
+    check_join_grad(gpu_lib, T, H, h, y, z, w, "channel", True, True, 0.0)
+
+
+@pytest.mark.parametrize("h,y,z,w", itertools.product(["float32", "bfloat16"], repeat=4))
+@pytest.mark.parametrize("T,H", [(40, 301), (3, 8200)])
+def test_every_type_with_every_other(gpu_lib, T, H, h, y, z, w):
+    check_join_grad(gpu_lib, T, H, h, y, z, w, "token", True, True, 0.0)
+
+
+@pytest.mark.parametrize("T,H,I,E,k", [(1, 33, 31, 4, 2), (4, 200, 600, 6, 2), (7, 1352, 336, 11, 3), (16, 257, 130, 9, 3),
+                                       (12, 1100, 544, 4, 3)])
+def test_pad_bytes_of_scales_are_not_used(gpu_lib, T, H, I, E, k):
+    case = _case(T, H, I, E, k)
+    (m1, v1), (m2, v2) = _mx4(case[3]), _mx4(case[4])
+    for m in (m1, m2):
+        blocks = (m.K + 31) // 32
+        assert m.scales.shape[-1] >= blocks
+        m.scales[..., blocks:] = 255
+    _check(_run(case, (m1, m2)), case, v1, v2, "float32")
+
+
+def test_two_streams_at_once(gpu_lib):
+    """Calls on two streams, each with scratch of its own, side by side."""
+    import torch
+
+    from paper_2609_07536_amd import block as K
+    cases = [_case(16, 512, 256, 16, 4), _case(3, 1024, 704, 8, 2)]
+    args = [(c[2].cuda(), _pack(c[3]), c[4].cuda(), torch.from_numpy(c[0]).cuda(), torch.from_numpy(c[1]).cuda()) for c in cases]
+    want = [K.layer_few(*a) for a in args]
+    w = torch.rand(1024, device="cuda")
+    x, dz = torch.randn(500, 1024, device="cuda"), torch.randn(500, 1024, device="cuda")
+    ref = K.join_grad(None, dz, x, before=w)
+    streams = [torch.cuda.Stream() for _ in args]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(20):
+        got = [[(K.layer_few(*a, stream=s), K.join_grad(None, dz, x, before=w, stream=s)) for a, s in zip(args, streams)]
+               for _ in range(3)]
+        torch.cuda.synchronize()
+        for each in got:
+            for (y, g), v in zip(each, want):
+                assert torch.equal(y, v) and torch.equal(g.h, ref.h) and torch.equal(g.before, ref.before)
