@@ -175,6 +175,9 @@ __global__ void __launch_bounds__(256) choose_kernel(const T* logits, const floa
 //   ... sigmoid            s q_e (1 - p_e) (g - G)
 //   sigmoid                s p_e (1 - p_e) g
 // An expert that several slots name enters by its number of slots `cnt` and their sum.
+// A token's logits, and in the end its gradients, stay in the registers of its lanes.  Bound by
+// latency at training's sizes (8192 tokens, 4 of 30 experts: 5.2 us for 2.2 MB, half of it the
+// launch).
 template <class T, int L, int R>
 __global__ void __launch_bounds__(256) choose_grad_kernel(const float* dgates, const T* logits, const int32_t* ids,
                                                           T* dlogits, long long first, int tokens, int E, int topk, bool softmax,
@@ -434,7 +437,9 @@ __device__ __forceinline__ void row_sums(float (&v)[n], float* lds) {
 }
 
 // A workgroup takes a row, U chunks of eight columns a thread, all of it in registers:
-// every tensor is read and written once.  Bound by memory.
+// every tensor is read and written once.  Bound by memory: 16384 rows of 2048, h, x and z in
+// bf16 and y in fp32, 59.4 us for 336 MB (5.6 TB/s; a large copy 4.9).  A few rows by latency: one
+// 2.6 us; 777 of 1352 with the norm after the block, a gate of tokens and dropout 5.9.
 template <int NT, int U>
 __global__ void __launch_bounds__(NT) join_kernel(JoinArgs a, long long first) {
   __shared__ float lds[NT / 64];
@@ -521,7 +526,10 @@ __global__ void __launch_bounds__(NT) join_kernel(JoinArgs a, long long first) {
 // that what a thread keeps fits its registers); its sums over rows of the columns'
 // gradients go to `parts` [array][G][H] and are added up by a second launch, always in the
 // same order.  Rows of up to 4096 columns keep these sums, and the weights, in registers;
-// longer ones (kLong) keep the sums in LDS and load weights and columns again.  Bound by memory.
+// longer ones (kLong) keep the sums in LDS and load weights and columns again.  Bound by memory:
+// 8192 rows of 2048 in bf16 with the norm before, 33.0 us and 4.6 for the second launch, 201 MB
+// (5.5 TB/s); 777 rows of 1351 in fp32 with everything, 14.2 and 4.1 for 23 MB: two rows a
+// workgroup, whose two sums over the row and random numbers stand one after the other.
 // Types are the kernel's own (B16: bf16, else fp32), so that a row is as few registers as it
 // is bytes; kY: with a norm after the block or a gate (else y is not read).
 template <bool B16>

@@ -17,7 +17,7 @@ namespace {
 
 constexpr int kMaxTopk = 64, kMaxExperts = 1024;
 constexpr int kMaxWidth = 1 << 22;   // H and I
-constexpr int kMaxShares = 8;        // workgroups that share a tile of the second launch
+constexpr int kMaxShares = 16;       // workgroups that share a tile of the second launch
 constexpr int kBlock = 32;   // elements of an mx4 block
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -296,7 +296,10 @@ __device__ __forceinline__ void put_act(const FewArgs& a, int unit, int t, int o
   p[a.pitch] = (__bf16)(fabsf(rest) < __builtin_inff() ? rest : 0.f);   // (of an infinity there is no rest)
 }
 
-// 64 packed columns (32 outputs), the waves taking every W-th 32 of K.
+// 64 packed columns (32 outputs), the waves taking every W-th 32 of K.  Bound by the stream of
+// the weights: 16 tokens, 32 experts of 2048 x 704, 34 us for 185 MB (5.4 TB/s); one token, 6
+// experts, 9.3 us for 35 MB, a quarter of it the launch (sixteen waves a workgroup, for twice
+// the loads under way: 9.3 too).
 constexpr int kCols = 64;
 template <int W>
 __global__ void __launch_bounds__(64 * W) few_up_kernel(FewArgs a) {
@@ -335,7 +338,10 @@ __global__ void __launch_bounds__(64 * W) few_up_kernel(FewArgs a) {
 }
 
 // 16 G outputs (their gate and their up rows), the waves taking every W-th 16 blocks of K.
-// R: rows of LDS for tokens.
+// R: rows of LDS for tokens.  One token, 6 experts of 2048 x 704: 7.3 us for 9 MB, one step a
+// wave, that is the launch and a chain of the choice, the loads and the sum over waves; 16
+// tokens, 32 experts: 16.2 us for 49 MB (3.0 TB/s), bound by the rows that go through LDS beside
+// the codes.
 template <int G, int R, int W, bool kOdd>
 __global__ void __launch_bounds__(64 * W) few_up_mx4_kernel(FewArgs a) {
   __shared__ float lds[W][16][32 * G];
@@ -475,20 +481,26 @@ __device__ __forceinline__ void join_sums(const FewArgs& a, const float (*lds)[1
   for (int i = threadIdx.x; i < a.T * COLS; i += 64 * W) {
     const int t = i / COLS, c = i % COLS, o = tile * COLS + c;
     if (o >= a.H) continue;
-    float part[kMaxShares], v = 0.f;   // (all of them on their way together)
+    const float* p = a.parts + (long long)t * a.H + o;
+    const long long pitch = (long long)a.T * a.H;
+    float part[8], v = 0.f;   // (eight of them on their way together)
+    for (int p0 = 0; p0 < a.shares; p0 += 8) {
 #pragma unroll
-    for (int p = 0; p < kMaxShares; ++p)
-      if (p < a.shares)
-        part[p] = __hip_atomic_load(a.parts + ((long long)p * a.T + t) * a.H + o, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      for (int i = 0; i < 8; ++i)
+        if (p0 + i < a.shares) part[i] = __hip_atomic_load(p + (p0 + i) * pitch, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 #pragma unroll
-    for (int p = 0; p < kMaxShares; ++p)
-      if (p < a.shares) v += part[p];
+      for (int i = 0; i < 8; ++i)
+        if (p0 + i < a.shares) v += part[i];
+    }
     put_out(a, t, o, v);
   }
 }
 
 // Up to eight tokens: rows 0 to 7 of the matrix instruction are one part of their
-// activations, rows 8 to 15 the other; more tokens (kMany): an instruction for each part.
+// activations, rows 8 to 15 the other; more tokens (kMany): an instruction for each part.  Bound
+// by the stream of the weights: 16 tokens, 32 experts of 2048 x 704, 22 us for 92 MB (4.2 TB/s);
+// one token, 6 experts, 7.6 us for 17 MB, where the launch, the list of the hit experts and the
+// shares' join are the most of it.
 template <int W, bool kMany>
 __global__ void __launch_bounds__(64 * W) few_down_kernel(FewArgs a) {
   __shared__ float lds[W][16][kCols];
@@ -563,7 +575,10 @@ __global__ void __launch_bounds__(64 * W) few_down_kernel(FewArgs a) {
 // Weights in mx4: 16 columns, a wave's step as in the first launch.  R tokens (up to eight)
 // at a time, rows 0 to 7 of the matrix instruction one part of their activations and rows 8
 // to 15 the other: the tokens that name the expert, one after the other, so that more than R
-// of them, which take another pass over the codes that are there, are rare.
+// of them, which take another pass over the codes that are there, are rare.  16 tokens, 32
+// experts of 2048 x 704: 13.7 us for 25 MB, one token 5.6 us: bound by latency, one to four steps
+// a wave between the list and the join (the next step's codes under way while a step is worked
+// on: equal, the other waves hide it).
 template <int R, int W, int kPasses>
 __global__ void __launch_bounds__(64 * W) few_down_mx4_kernel(FewArgs a) {
   __shared__ float lds[W][16][16];
@@ -644,13 +659,15 @@ size_t up16(size_t n) { return (n + 15) / 16 * 16; }
 
 // The second launch: columns of a tile, waves of a workgroup, and the shares of a tile's
 // work: as many as there are CUs for, while every wave keeps a step.  (us, 32 experts, top 6,
-// 2048 x 704: bf16, one token 12.6, 6.6, 6.5 with 1, 4, 8 shares, 16 tokens 77, 24, 18; mx4, 16
-// tokens 14.3, 10.4, 13.0 with 1, 2, 4, and 5 tokens of 11 experts of 1352 x 336 4.6 and 6.3
-// with 1 and 2, half of the waves without a step.)
+// 2048 x 704: bf16, one token 12.6, 9.6, 7.8, 7.6 with 1, 2, 4, 8 shares, 16 tokens 96, 54, 31,
+// 22; mx4, 16 tokens 17.7 and 13.7 with 1 and 2.)  Sixteen only with four steps a wave, and
+// slots enough that most units are hit: the whole layer, 32 experts, top 8, 1024 x 512 in bf16,
+// with 8 and 16: one token 13.7 and 15.5, five 21.6 and 22.7, eight 26.7 and 25.2, sixteen 32.9
+// and 30.8.
 struct Down {
   int cols, waves, tiles, shares;
 };
-Down down_of(bool mx4, int T, int H, int I, int units) {
+Down down_of(bool mx4, int T, int H, int I, int units, int topk) {
   Down d;
   d.cols = mx4 ? 16 : kCols;
   d.waves = mx4 && T <= 4 ? 16 : 8;
@@ -658,7 +675,8 @@ Down down_of(bool mx4, int T, int H, int I, int units) {
   const int k = mx4 ? kStepK : 32;
   const long long steps = (long long)units * ((I + k - 1) / k);
   d.shares = 1;
-  while (d.shares < kMaxShares && 2 * d.shares * d.tiles <= 256 && steps >= 2 * d.shares * d.waves) d.shares *= 2;
+  while (d.shares < 8 && 2 * d.shares * d.tiles <= 256 && steps >= 2 * d.shares * d.waves) d.shares *= 2;
+  if (d.shares == 8 && 16 * d.tiles <= 256 && steps >= 64 * d.waves && T * topk >= 2 * units) d.shares = kMaxShares;
   return d;
 }
 
@@ -674,7 +692,7 @@ Layout layout_of(int T, int H, int I, int E, int topk) {
   l.parts = l.count + up16((size_t)(H + 15) / 16 * sizeof(uint32_t));
   size_t parts = 0;
   for (const bool mx4 : {false, true}) {
-    const Down d = down_of(mx4, T, H, I, (int)units);
+    const Down d = down_of(mx4, T, H, I, (int)units, topk);
     const size_t n = d.shares > 1 ? (size_t)d.shares * T * H * sizeof(float) : 0;
     parts = n > parts ? n : parts;
   }
@@ -715,12 +733,12 @@ int few(bool mx4, const void* hidden, const void* w1, const void* w1_scales, con
   a.parts = (float*)((char*)scratch + l.parts);
   a.T = T, a.H = H, a.I = I, a.E = E, a.topk = topk, a.first = first;
   a.slots = T * topk, a.units = units, a.pitch = act_pitch(I), a.out16 = out_type == MOE_BF16;
-  const Down d = down_of(mx4, T, H, I, units);
+  const Down d = down_of(mx4, T, H, I, units, topk);
   a.out_tiles = d.tiles, a.shares = d.shares;
   const hipStream_t s = (hipStream_t)stream;
   // Variants by the rows that tokens take in LDS (which bounds how many waves a CU holds), and
   // beyond eight tokens two waves a workgroup, with two tiles where K is long (16 tokens: H =
-  // 2048 17.9 us with one tile and 15.6 with two, H = 1024 8.8 and 10.3).
+  // 2048 18.8 us with one tile and 16.2 with two, H = 1024 10.2 and 11.1).
   const bool odd = H % kBlock != 0;
   if (!mx4) {
     a.tiles = (2 * I + kCols - 1) / kCols;

@@ -157,3 +157,14 @@ def test_two_streams_at_once(gpu_lib):
         for each in got:
             for (y, g), v in zip(each, want):
                 assert torch.equal(y, v) and torch.equal(g.h, ref.h) and torch.equal(g.before, ref.before)
+
+
+@pytest.mark.parametrize("T,H,I,E,k,mx4", [(8, 1024, 512, 32, 8, False), (16, 200, 1056, 40, 5, False), (9, 1000, 528, 32, 8, False),
+                                           (16, 130, 8200, 36, 5, True), (8, 256, 8192, 32, 8, True)])
+def test_narrow_layers_with_many_slots(gpu_lib, T, H, I, E, k, mx4):
+    """Few columns of out, long sums: sixteen workgroups share a tile of the second launch."""
+    case = _case(T, H, I, E, k)
+    (m1, v1), (m2, v2) = (_mx4(case[3]), _mx4(case[4])) if mx4 else ((_pack(case[3]), case[3].double().numpy()), (case[4].cuda(), case[4].double().numpy()))
+    got = _run(case, (m1, m2))
+    _check(got, case, v1, v2, "float32")
+    assert np.array_equal(got, _run(case, (m1, m2)))
