@@ -337,63 +337,96 @@ __global__ void __launch_bounds__(64 * W) few_up_kernel(FewArgs a) {
   if (tile == 0) write_hit(a, unit, e, tokens);
 }
 
-// 16 G outputs (their gate and their up rows), the waves taking every W-th 16 blocks of K.
-// R: rows of LDS for tokens.  One token, 6 experts of 2048 x 704: 7.3 us for 9 MB, one step a
-// wave, that is the launch and a chain of the choice, the loads and the sum over waves; 16
-// tokens, 32 experts: 16.2 us for 49 MB (3.0 TB/s), bound by the rows that go through LDS beside
-// the codes.
-template <int G, int R, int W, bool kOdd>
+// 16 outputs (their gate and their up rows), the waves taking every W-th 16 blocks of K.
+// R: rows of LDS for tokens.  With more than eight tokens (kMany) those that name the expert, R
+// at a time, each R another pass over the expert's codes: more than seven of sixteen are rare,
+// and a row for each of sixteen leaves a CU half of the waves (11 experts of 1352 x 336, whole
+// layer of 9 and 16 tokens 15.2 and 16.5 us so, 12.1 and 13.2 now; 32 of 2048 x 704 27.2 and 29.6,
+// 26.2 and 29.1; 1024 x 512, top 8, 16 tokens 17.2 and 17.8; all passes on registers in one loop
+// 30 and more).  One token, 6 experts of 2048 x 704: 7.3 us for 9 MB, one step a wave, that is
+// the launch and a chain of the choice, the loads and the sum over waves; 8 tokens, 24 experts:
+// some 15 us for 37 MB.
+template <int R, int W, bool kMany, bool kOdd>
 __global__ void __launch_bounds__(64 * W) few_up_mx4_kernel(FewArgs a) {
   // (a wave's sums take the place of its rows, so that a CU holds four workgroups of R = 8
-  // instead of three: the layer of 8 tokens, 32 experts of 1024 x 512, top 8, 19.7 -> 16.4 us)
-  __shared__ __attribute__((aligned(16))) uint8_t lds[W][R * kStepBytes];
-  static_assert(R * kStepBytes >= 16 * 32 * G * (int)sizeof(float), "room for the sums");
+  // instead of three: the layer of 8 tokens, 32 experts of 1024 x 512, top 8, 19.7 -> 16.4 us;
+  // with kMany they are needed while rows are)
+  constexpr int kSums = 16 * 32 * (int)sizeof(float), kRows = R * kStepBytes;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[W][kMany ? kRows + kSums : kRows];
+  static_assert(kRows >= kSums, "room for the sums");
   int unit, tile, e;
   uint32_t tokens;
   if (!begin_up(a, &unit, &tile, &e, &tokens)) return;
   const int wave = threadIdx.x >> 6, n = threadIdx.x & 15;
   uint8_t* const rows = lds[wave];
-  const int KB = (a.H + kBlock - 1) / kBlock, KS = (KB + 3) / 4 * 4, col = tile * 16 * G + n;
+  const int KB = (a.H + kBlock - 1) / kBlock, KS = (KB + 3) / 4 * 4, col = tile * 16 + n;
   const long long codes = 2LL * a.I * KB * 16, scales = 2LL * a.I * KS;
   const Buffer wc = buffer(a.w1 + e * codes, codes), ws = buffer(a.w1_scales + e * scales, scales);
-  f32x4 acc[2 * G] = {};   // gate and up of the first 16 columns, of the next, ...
-  bool bad[2 * G] = {};
-  const int token = min(n, R - 1);
-  for (int kb0 = wave * kStepBlocks; kb0 < KB; kb0 += W * kStepBlocks) {
-    Mx4Step<2 * G> b;
-    // (rows of tokens that do not name the expert hold anything: they make results that nobody takes)
-    rows_read();
-    const i32x4 rsrc = buffer_rsrc(a.x, 2LL * a.T * a.H);
-    for (uint32_t m = tokens; m; m &= m - 1) {
-      const int t = __builtin_ctz(m);
-      row_to_lds<kOdd>(rows + t * kStepBytes, rsrc, a.x, t * a.H, kb0 * kBlock, a.H);
+  const i32x4 rsrc = buffer_rsrc(a.x, 2LL * a.T * a.H);
+  float (*const sums)[32] = (float (*)[32])(kMany ? rows + kRows : rows);
+  const int row = min(n, R - 1);
+  uint32_t left = tokens;
+#pragma unroll 1
+  do {
+    // up to R tokens, those with the R lowest numbers (kMany), each in a row of its own
+    uint32_t these = left;
+    if (kMany) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) left &= left - 1;
+      these &= ~left;
     }
-#pragma unroll
-    for (int m = 0; m < 2 * G; ++m) {
-      const int c = col + m / 2 * 16;
-      b.load(m, wc, ws, c + m % 2 * a.I, kb0, KB, KS, c < a.I);
-    }
-    waitcnt_vm<0>();
-    asm volatile("" ::: "memory");
-    b.align(kb0, KB, KS);
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const u32x4 v = row_operand(rows, token, j, q);
-#pragma unroll
-        for (int m = 0; m < 2 * G; ++m) acc[m] = mfma(v, b.eight(m, j, q), acc[m]);
+    f32x4 acc[2] = {};   // gate and up
+    bool bad[2] = {};
+    for (int kb0 = wave * kStepBlocks; kb0 < KB; kb0 += W * kStepBlocks) {
+      Mx4Step<2> b;
+      // (rows of tokens that do not name the expert hold anything: they make results that nobody takes)
+      rows_read();
+      int r = 0;
+      for (uint32_t m = these; m; m &= m - 1, ++r) {
+        const int t = __builtin_ctz(m);
+        row_to_lds<kOdd>(rows + (kMany ? r : t) * kStepBytes, rsrc, a.x, t * a.H, kb0 * kBlock, a.H);
       }
 #pragma unroll
-    for (int m = 0; m < 2 * G; ++m) bad[m] |= b.bad(m);
-  }
+      for (int m = 0; m < 2; ++m) b.load(m, wc, ws, col + m * a.I, kb0, KB, KS, col < a.I);
+      waitcnt_vm<0>();
+      asm volatile("" ::: "memory");
+      b.align(kb0, KB, KS);
 #pragma unroll
-  for (int m = 0; m < 2 * G; ++m) put_column((float (*)[32 * G])rows, 16 * m + n, with_nan(acc[m], bad[m]));
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const u32x4 v = row_operand(rows, row, j, q);
+#pragma unroll
+          for (int m = 0; m < 2; ++m) acc[m] = mfma(v, b.eight(m, j, q), acc[m]);
+        }
+#pragma unroll
+      for (int m = 0; m < 2; ++m) bad[m] |= b.bad(m);
+    }
+#pragma unroll
+    for (int m = 0; m < 2; ++m) acc[m] = with_nan(acc[m], bad[m]);
+    if (kMany) {
+      int token[4] = {-1, -1, -1, -1};   // of the lane's rows 4 g + i
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const int t = these ? __builtin_ctz(these) : -1;
+        these &= these - 1;
+        token[r % 4] = r / 4 == (threadIdx.x & 63) >> 4 ? t : token[r % 4];
+      }
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (token[i] >= 0) sums[token[i]][16 * m + n] = acc[m][i];
+    } else {
+#pragma unroll
+      for (int m = 0; m < 2; ++m) put_column(sums, 16 * m + n, acc[m]);
+    }
+  } while (kMany && left);
   __syncthreads();
-  for (int i = threadIdx.x; i < 256 * G; i += 64 * W) {
-    const int t = i / (16 * G), c = i % (16 * G), o = tile * 16 * G + c, at = c / 16 * 32 + c % 16;
+  for (int i = threadIdx.x; i < 256; i += 64 * W) {
+    const int t = i / 16, c = i % 16, o = tile * 16 + c;
     if (((tokens >> t) & 1) && o < a.pitch)
-      put_act(a, unit, t, o, o < a.I ? swiglu<W, 32 * G>((const float*)lds[0], R * kStepBytes / 4, t, at, at + 16) : 0.f);
+      put_act(a, unit, t, o, o < a.I ? swiglu<W, 32>(sums[0] - wave * (int)(sizeof(lds[0]) / 4), sizeof(lds[0]) / 4, t, c, c + 16) : 0.f);
   }
   if (tile == 0) write_hit(a, unit, e, tokens);
 }
@@ -739,21 +772,18 @@ int few(bool mx4, const void* hidden, const void* w1, const void* w1_scales, con
   const Down d = down_of(mx4, T, H, I, units, topk);
   a.out_tiles = d.tiles, a.shares = d.shares;
   const hipStream_t s = (hipStream_t)stream;
-  // Variants by the rows that tokens take in LDS (which bounds how many waves a CU holds), and
-  // beyond eight tokens two waves a workgroup, with two tiles where K is long (16 tokens: H =
-  // 2048 18.8 us with one tile and 16.2 with two, H = 1024 10.2 and 11.1).
+  // Variants by the rows that tokens take in LDS, which bounds how many waves a CU holds; seven
+  // with the sums beside them are what four workgroups of the first launch have room for.
   const bool odd = H % kBlock != 0;
   if (!mx4) {
     a.tiles = (2 * I + kCols - 1) / kCols;
     few_up_kernel<8><<<(unsigned)(units * a.tiles), 64 * 8, 0, s>>>(a);
   } else {
-    const int groups = T > 8 && H > 1024 ? 2 : 1, waves = T > 8 ? 2 : 4;
-    a.tiles = (a.pitch + 16 * groups - 1) / (16 * groups);
-    auto up = T <= 4      ? (odd ? few_up_mx4_kernel<1, 4, 4, true> : few_up_mx4_kernel<1, 4, 4, false>)
-              : T <= 8    ? (odd ? few_up_mx4_kernel<1, 8, 4, true> : few_up_mx4_kernel<1, 8, 4, false>)
-              : groups > 1 ? (odd ? few_up_mx4_kernel<2, 16, 2, true> : few_up_mx4_kernel<2, 16, 2, false>)
-                           : (odd ? few_up_mx4_kernel<1, 16, 2, true> : few_up_mx4_kernel<1, 16, 2, false>);
-    up<<<(unsigned)(units * a.tiles), 64 * waves, 0, s>>>(a);
+    a.tiles = a.pitch / 16;
+    auto up = T <= 4   ? (odd ? few_up_mx4_kernel<4, 4, false, true> : few_up_mx4_kernel<4, 4, false, false>)
+              : T <= 8 ? (odd ? few_up_mx4_kernel<8, 4, false, true> : few_up_mx4_kernel<8, 4, false, false>)
+                       : (odd ? few_up_mx4_kernel<7, 4, true, true> : few_up_mx4_kernel<7, 4, true, false>);
+    up<<<(unsigned)(units * a.tiles), 64 * 4, 0, s>>>(a);
   }
   if (hipGetLastError() != hipSuccess) return MOE_ERR_HIP;
   auto down = !mx4     ? (T <= 8 ? few_down_kernel<8, false> : few_down_kernel<8, true>)

@@ -168,3 +168,15 @@ def test_narrow_layers_with_many_slots(gpu_lib, T, H, I, E, k, mx4):
     got = _run(case, (m1, m2))
     _check(got, case, v1, v2, "float32")
     assert np.array_equal(got, _run(case, (m1, m2)))
+
+
+@pytest.mark.parametrize("T,H,I,E,k", [(16, 1351, 50, 2, 2), (15, 64, 600, 3, 3), (9, 33, 31, 2, 2), (14, 2080, 40, 1, 1), (16, 520, 65, 20, 18)])
+def test_every_token_on_the_same_experts_in_4_bits(gpu_lib, T, H, I, E, k):
+    """More tokens of an expert than one pass over its codes takes, and a NaN block."""
+    case = _case(T, H, I, E, k)
+    (m1, v1), (m2, v2) = _mx4(case[3]), _mx4(case[4])
+    _check(_run(case, (m1, m2)), case, v1, v2, "float32")
+    m1.scales[case[0][T - 1, 0], I + 3, 0] = 255      # (a row of the up projection)
+    got = _run(case, (m1, m2))
+    named = (case[0] == case[0][T - 1, 0]).any(1)
+    assert np.isnan(got[named]).all() and np.isfinite(got[~named]).all()
