@@ -1067,11 +1067,12 @@ extern "C" int moe_join_grad(const void* dx, const void* dz, const void* x, cons
   if (bad) return bad;
   if ((d_after && !after) || (d_before && !before) || (d_gate && gate_kind == MOE_GATE_NONE)) return MOE_ERR_INVALID_ARG;
   if (T > 0 && ((!dx && !dz) || (dz && (!before || !x)) || (dy && !y))) return MOE_ERR_INVALID_ARG;
-  for (const void* o : {(const void*)dh, (const void*)dy, (const void*)d_after, (const void*)d_gate, (const void*)d_before})
-    for (const void* in : {dx, dz, x, y, after, gate, before, (const void*)rng})
-      if (same(o, in) && !(o == dh && in == dx)) return MOE_ERR_INVALID_ARG;
-  if (same(dh, dx) && dx == dz) return MOE_ERR_INVALID_ARG;
   const void* outs[5] = {dh, dy, d_after, d_gate, d_before};
+  for (const void* o : outs)
+    for (const void* in : {dz, x, y, after, gate, before, (const void*)rng})
+      if (same(o, in)) return MOE_ERR_INVALID_ARG;
+  for (int i = 1; i < 5; ++i)   // (dh may be dx)
+    if (same(outs[i], dx)) return MOE_ERR_INVALID_ARG;
   for (int i = 0; i < 5; ++i)
     for (int j = 0; j < i; ++j)
       if (same(outs[i], outs[j])) return MOE_ERR_INVALID_ARG;

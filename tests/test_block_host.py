@@ -223,3 +223,14 @@ def test_a_differentiable_norm_alone_refuses_what_it_would_leave_out():
             A.join(x, **bad)
     with pytest.raises(TypeError):
         A.join(None, before=w)
+
+
+def test_join_grad_in_place_only_of_dx():
+    """dh may be dx, and nothing else: also where dx has that other input's address.  (Without
+    scratch no call gets past its checks.)"""
+    inputs = dict(dz=2 * P, x=3 * P, y=4 * P, after=5 * P, gate=6 * P, before=7 * P, rng=8 * P)
+    for name in inputs:
+        assert _grad(dh=P, scratch=None, **{name: P}) == B.MOE_ERR_INVALID_ARG, name
+        assert _grad(dx=inputs[name], dh=inputs[name], scratch=None) == B.MOE_ERR_INVALID_ARG, name
+    assert _grad(dh=P, x=P, y=P, scratch=None) == B.MOE_ERR_INVALID_ARG
+    assert _grad(dh=P, scratch=None) == B.MOE_ERR_WORKSPACE
