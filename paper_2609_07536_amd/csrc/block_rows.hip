@@ -1036,9 +1036,9 @@ extern "C" int moe_join(const void* h, const void* y, const void* after, const v
   if ((!h && !y) || (y && !x) || (before && !z) || (!y && !before)) return MOE_ERR_INVALID_ARG;
   if (!y) a.x = nullptr;
   if (!before) a.z = nullptr;
-  for (const void* in : {h, y, after, gate, before, (const void*)rng})
-    if (same(a.z, in) || (in != h && same(a.x, in))) return MOE_ERR_INVALID_ARG;
-  if (same(a.x, a.z) || (same(a.x, h) && h == y)) return MOE_ERR_INVALID_ARG;
+  for (const void* in : {y, after, gate, before, (const void*)rng})   // (x may be h)
+    if (same(a.z, in) || same(a.x, in)) return MOE_ERR_INVALID_ARG;
+  if (same(a.z, h) || same(a.x, a.z)) return MOE_ERR_INVALID_ARG;
   set_common(&a, T, H, h_type, y_type, z_type, w_type, gate_kind, scale, drop, eps);
   const hipStream_t s = (hipStream_t)stream;
   with_row(H, [&](auto shape) {

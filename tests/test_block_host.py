@@ -234,3 +234,10 @@ def test_join_grad_in_place_only_of_dx():
         assert _grad(dx=inputs[name], dh=inputs[name], scratch=None) == B.MOE_ERR_INVALID_ARG, name
     assert _grad(dh=P, x=P, y=P, scratch=None) == B.MOE_ERR_INVALID_ARG
     assert _grad(dh=P, scratch=None) == B.MOE_ERR_WORKSPACE
+
+
+def test_join_in_place_only_of_h():
+    """x may be h, and nothing else: also where h has that other input's address."""
+    for name in ("y", "after", "gate", "before", "rng"):
+        assert _join(x=P, **{name: P}) == B.MOE_ERR_INVALID_ARG, name
+        assert _join(z=P, **{name: P}) == B.MOE_ERR_INVALID_ARG, name
