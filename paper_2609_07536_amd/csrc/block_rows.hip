@@ -403,14 +403,15 @@ struct JoinArgs {
   bool drop;
 };
 
-// v times the dropout's factor, columns c .. c + 7 of row t (c a multiple of 8)
-__device__ __forceinline__ void drop8(const JoinArgs& a, uint64_t seed, uint64_t offset, long long t, int c,
-                                      float (&v)[8]) {
+// x + factor drop(v), columns c .. c + 7 of row t (c a multiple of 8): where it drops x stays,
+// also with a factor that is no finite number (a gate of tokens is in it).
+__device__ __forceinline__ void drop8(const JoinArgs& a, uint64_t seed, uint64_t offset, long long t, int c, float factor,
+                                      const float (&v)[8], float (&x)[8]) {
   uint32_t w[4];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     if (i % 4 == 0) philox((uint32_t)(c / 4 + i / 4), (uint32_t)t, offset, seed, w);
-    v[i] = w[i % 4] >= a.least ? v[i] * a.keep : 0.f;
+    x[i] = w[i % 4] >= a.least ? fmaf(factor, v[i] * a.keep, x[i]) : x[i];
   }
 }
 
@@ -492,9 +493,11 @@ __global__ void __launch_bounds__(NT) join_kernel(JoinArgs a, long long first) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] *= w[i];
       }
-      if (a.drop) drop8(a, seed, offset, t, c, v);
+      if (a.drop)
+        drop8(a, seed, offset, t, c, factor, v, x[u]);
+      else
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[u][i] = fmaf(factor, v[i], x[u][i]);
+        for (int i = 0; i < 8; ++i) x[u][i] = fmaf(factor, v[i], x[u][i]);
       const Raw o = raw(x[u], a.h16);
       store8(a.x, a.h16, row + c, n[u], o);
       if (a.h16) {   // the norm's x is the one that is kept

@@ -293,3 +293,23 @@ def test_dropout_depends_on_seed_offset_row_and_column_alone(gpu_lib):
     # the gradient of a dropout is the same call on the gradient
     d = torch.randn_like(x)
     assert torch.equal(K.join_grad(d, None, None, x, drop=0.3, rng=rng, residual=False).y, K.join(None, d, drop=0.3, rng=rng).h)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_dropped_elements_take_nothing_from_an_infinite_gate(gpu_lib, dtype):
+    """drop(a) is 0 where it drops, whatever a token's gate is: h goes on as it is there, to
+    the bit, and what is kept is infinite."""
+    import torch
+    K = _K()
+    T, H, p = 6, 700, 0.4
+    rng = np.random.default_rng(5)
+    h, y = _cuda(rng.standard_normal((T, H)), dtype), _cuda(rng.standard_normal((T, H)), dtype)
+    gate = torch.ones(T, 1, device="cuda")
+    gate[1], gate[4] = float("inf"), float("nan")
+    kept = torch.from_numpy(ob.kept(3, 8, T, H, p) != 0).cuda()
+    for y_h in (h, None):
+        x = K.join(y_h, y, gate=gate, drop=p, rng=torch.tensor([3, 8], device="cuda")).h
+        base = torch.zeros_like(y) if y_h is None else h
+        assert torch.equal(x[~kept], base[~kept])
+        assert bool(x[1][kept[1]].isinf().all()) and bool(x[4][kept[4]].isnan().all())
+        assert bool(x[[0, 2, 3, 5]].isfinite().all())
