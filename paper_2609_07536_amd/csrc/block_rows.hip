@@ -967,7 +967,7 @@ int threads_of(S, int H, int each) {
 // small beside the rows.
 int grad_groups(int T, int H) {
   const int most = H <= 256 ? 2048 : H <= 1024 ? 1024 : H <= 2048 ? 512 : 256;
-  const int rows = (T + 1) / 2;   // two rows a workgroup, where there are few
+  const int rows = T / 2 + T % 2;   // two rows a workgroup, where there are few
   return rows < most ? (rows < 1 ? 1 : rows) : most;
 }
 

@@ -241,3 +241,10 @@ def test_join_in_place_only_of_h():
     for name in ("y", "after", "gate", "before", "rng"):
         assert _join(x=P, **{name: P}) == B.MOE_ERR_INVALID_ARG, name
         assert _join(z=P, **{name: P}) == B.MOE_ERR_INVALID_ARG, name
+
+
+def test_scratch_of_the_most_rows_there_can_be():
+    """2^31 - 1 rows fill the card's workgroups as 2^31 - 2 do; one of them would add up all
+    rows alone."""
+    for H in (1, 300, 16384):
+        assert K.join_grad_scratch_size(2 ** 31 - 1, H) == K.join_grad_scratch_size(2 ** 31 - 2, H) > 0
