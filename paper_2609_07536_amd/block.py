@@ -218,7 +218,8 @@ def join(h, y=None, after=None, gate=None, scale: float = 1.0, drop: float = 0.0
       drop           dropout's probability; rng: int64 [2] on the GPU, seed and offset,
                      read as the call runs (a program gives every call numbers of its own)
     h None: nothing to add to (the result is of y's type).  y None: h's norm alone.
-    out: where both go (out.h may be h itself; out.z None without `before`)."""
+    out: where both go (out.h may be h itself, and without y is it or None; out.z None
+    without `before`)."""
     if h is None and y is None:
         raise TypeError("expected h, y or both")
     L, (device, handle) = lib(), _here(stream)
@@ -237,8 +238,14 @@ def join(h, y=None, after=None, gate=None, scale: float = 1.0, drop: float = 0.0
     x, z = out
     if y is not None:
         _fits(x, "out.h", shape, (h_type,), device)
+    elif x is not h:
+        if x is not None and x.data_ptr() != h.data_ptr():
+            raise TypeError("out.h: without y the stream goes on in h; expected None or h")
+        out = Joined(h, z)
     if before is not None:
         _fits(z, "out.z", shape, _FLOAT, device)
+    elif z is not None:
+        raise TypeError("out.z: there is no norm without `before`; expected None")
     r = L.moe_join(_ptr(h), _ptr(y), _ptr(after), _ptr(gate), _ptr(before), seeds,
                    None if y is None else x.data_ptr(), None if before is None else z.data_ptr(), T, H,
                    _TYPES[h_type], 0 if y is None else _TYPES[y.dtype], 0 if before is None else _TYPES[z.dtype],

@@ -313,3 +313,21 @@ def test_dropped_elements_take_nothing_from_an_infinite_gate(gpu_lib, dtype):
         assert torch.equal(x[~kept], base[~kept])
         assert bool(x[1][kept[1]].isinf().all()) and bool(x[4][kept[4]].isnan().all())
         assert bool(x[[0, 2, 3, 5]].isfinite().all())
+
+
+def test_join_refuses_outputs_that_it_would_not_write(gpu_lib):
+    """Without y the stream goes on in h, and without `before` there is no norm: a place for
+    them would be returned as it was."""
+    import torch
+    K = _K()
+    h, w = torch.randn(3, 40, device="cuda"), torch.rand(40, device="cuda")
+    z, other = torch.empty_like(h), torch.full_like(h, 7.0)
+    with pytest.raises(TypeError, match="out.h"):
+        K.join(h, before=w, out=K.Joined(other, z))
+    with pytest.raises(TypeError, match="out.z"):
+        K.join(h, h.clone(), out=K.Joined(torch.empty_like(h), other))
+    assert bool((other == 7.0).all())
+    want = K.join(h, before=w, dtype=torch.float32)
+    for place in (h, None, h.view(3, 40)):
+        got = K.join(h, before=w, out=K.Joined(place, z))
+        assert got.h.data_ptr() == h.data_ptr() and got.z is z and torch.equal(z, want.z)
