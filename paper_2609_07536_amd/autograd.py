@@ -101,7 +101,7 @@ class _Join(torch.autograd.Function):
     def forward(ctx, h, y, after, gate, before, scale, drop, rng, eps, dtype):
         h, y, after, gate, before = (t if t is None else t.contiguous() for t in (h, y, after, gate, before))
         # (a copy: the program may write the next call's numbers to its own before the backward pass)
-        rng = rng.clone() if drop else None
+        rng = rng.clone() if drop and rng is not None else None
         x, z = K.join(h, y, after, gate, scale, drop, rng, before, eps, dtype=dtype)
         # y is read again for a norm after the block or a gate, the stream for the norm before
         ctx.save_for_backward(y if after is not None or gate is not None else None, after, gate, before, rng,

@@ -248,3 +248,12 @@ def test_scratch_of_the_most_rows_there_can_be():
     rows alone."""
     for H in (1, 300, 16384):
         assert K.join_grad_scratch_size(2 ** 31 - 1, H) == K.join_grad_scratch_size(2 ** 31 - 2, H) > 0
+
+
+def test_a_differentiable_join_with_dropout_refuses_to_go_without_numbers():
+    from paper_2609_07536_amd import autograd as A
+    x = torch.zeros(4, 8)
+    with pytest.raises(TypeError):
+        A.join(x, x, drop=0.5)
+    with pytest.raises(TypeError):
+        K.join(x, x, drop=0.5)

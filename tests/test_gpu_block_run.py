@@ -300,3 +300,12 @@ def test_example(gpu_lib):
     assert len(losses) == 3 and all(np.isfinite(losses))
     for name, p in blocks.named_parameters():
         assert p.grad is not None and bool(torch.isfinite(p.grad).all()) and float(p.grad.abs().max()) > 0, name
+
+
+def test_differentiable_join_refuses_dropout_without_numbers(gpu_lib):
+    import torch
+
+    from paper_2609_07536_amd import autograd as A
+    x = torch.zeros(4, 8, device="cuda")
+    with pytest.raises(TypeError, match="rng: dropout needs one"):
+        A.join(x, x, drop=0.5)
