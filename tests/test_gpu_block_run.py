@@ -309,3 +309,42 @@ def test_differentiable_join_refuses_dropout_without_numbers(gpu_lib):
     x = torch.zeros(4, 8, device="cuda")
     with pytest.raises(TypeError, match="rng: dropout needs one"):
         A.join(x, x, drop=0.5)
+
+
+@pytest.mark.parametrize("used", ["z", "x", "both"])
+@pytest.mark.parametrize("kind", ["norm alone", "none", "token", "channel"])
+def test_differentiable_join_by_what_is_used(gpu_lib, used, kind):
+    """Every leaf's gradient where the stream alone, its norm alone, or both are used, of the
+    join and of the norm alone, against torch's own operations in 64 bits: in fp32, within the
+    1e-4 of test_differentiable_join's sizes.  A leaf that what is used does not depend on
+    has zeros or no gradient."""
+    import torch
+
+    from paper_2609_07536_amd import autograd as A
+    gen = torch.Generator(device="cuda").manual_seed(6)
+
+    def leaf(*shape):
+        return torch.randn(shape, device="cuda", generator=gen)
+    T, H, with_y = 50, 130, kind != "norm alone"
+    leaves = dict(h=leaf(T, H), y=leaf(T, H) if with_y else None, after=1 + leaf(H) / 4 if with_y else None,
+                  gate={"token": leaf(T, 1), "channel": leaf(1, H)}.get(kind), before=1 + leaf(H) / 4)
+    a = {k: None if v is None else v.clone().requires_grad_() for k, v in leaves.items()}
+    b = {k: None if v is None else v.double().requires_grad_() for k, v in leaves.items()}
+    x, z = A.join(a["h"], a["y"], a["after"], a["gate"], scale=0.7 if with_y else 1.0, before=a["before"], dtype=torch.float32)
+    wx = b["h"]
+    if with_y:
+        c = b["y"] * torch.rsqrt(b["y"].square().mean(1, keepdim=True) + 1e-6) * b["after"]
+        wx = wx + 0.7 * (c if b["gate"] is None else c * b["gate"])
+    wz = wx * torch.rsqrt(wx.square().mean(1, keepdim=True) + 1e-6) * b["before"]
+    dx, dz = leaf(T, H) * (used != "z"), leaf(T, H) * (used != "x")
+    (((x * dx).sum() if used != "z" else 0.0) + ((z * dz).sum() if used != "x" else 0.0)).backward()
+    ((wx * dx.double()).sum() + (wz * dz.double()).sum()).backward()
+    for k in a:
+        if a[k] is None:
+            continue
+        want = b[k].grad
+        if not bool(want.any()):
+            assert used == "x" and k == "before" and (a[k].grad is None or not bool(a[k].grad.any()))
+            continue
+        off = (a[k].grad.double() - want).abs().max() / want.abs().max()
+        assert off <= 1e-4, (k, float(off))
