@@ -93,9 +93,10 @@ size_t moe_join_grad_scratch_size(int32_t T, int32_t H);
  *   dx       [T, H] of h_type
  *   dz       [T, H] of z_type (with before)
  *   x        [T, H] of h_type as moe_join wrote it (without y: h); read with dz only
- *   y        [T, H] of y_type, or NULL as in the join; read with after or a gate only
+ *   y        [T, H] of y_type, or NULL as in the join; read with after or a gate only,
+ *            and may be NULL without them also where the join had one
  *   dh       [T, H] of h_type, may be dx; NULL: not written
- *   dy       [T, H] of y_type (with y); NULL: not written
+ *   dy       [T, H] of y_type (where the join had y); NULL: not written
  *   d_after, d_before   fp32 [H]; NULL: not written
  *   d_gate   fp32 [T] or [H]; NULL: not written
  * Apart from dh = dx outputs overlap neither inputs nor each other.  The columns'

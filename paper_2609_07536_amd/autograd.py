@@ -121,16 +121,16 @@ class _Join(torch.autograd.Function):
             return (None,) * 10
         d_x, d_z = (d if d is None else d.contiguous() for d in (d_x, d_z))
         some = d_x if d_x is not None else d_z
-        if y is None and y_type is not None:
-            y = some.new_empty(some.shape, dtype=y_type)   # (its type alone matters)
         need = ctx.needs_input_grad
 
         def room(wanted, shape, dtype):
             return some.new_empty(shape, dtype=dtype) if wanted else None
-        out = K.JoinGrads(room(residual and need[0], some.shape, x_type), room(y is not None and need[1], some.shape, y_type),
+        out = K.JoinGrads(room(residual and need[0], some.shape, x_type), room(y_type is not None and need[1], some.shape, y_type),
                           room(after is not None and need[2], some.shape[1:], torch.float32),
                           room(gate is not None and need[3], gate.shape if gate is not None else (), torch.float32),
                           room(before is not None and need[4], some.shape[1:], torch.float32))
+        if y is None and out.y is None:
+            drop = 0.0   # (nothing that is asked for goes through it)
         K.join_grad(d_x, d_z, x, y, after, gate, scale, drop, rng, before, eps, out=out)
         grads = [g if g is None or t is None else g.to(t.dtype) for g, t in zip(out[2:], (after, gate, before))]
         return (*out[:2], *grads) + (None,) * 5

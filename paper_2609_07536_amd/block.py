@@ -271,7 +271,8 @@ def join_grad(d_h, d_z, h, y=None, after=None, gate=None, scale: float = 1.0, dr
     type) and d_z [T, H] (either may be None), its other arguments as they were, and h,
     the stream as join returned it (read with d_z only).  residual False: join had no h
     (no gradient of it).  out: where the gradients go, None for ones that are not wanted
-    (out.h may be d_h).  scratch: uint8, at least join_grad_scratch_size bytes."""
+    (out.h may be d_h).  y is read with `after` or a gate only: without them out.y alone
+    says that there was one, and its type.  scratch: uint8, at least join_grad_scratch_size bytes."""
     some = d_h if d_h is not None else h
     if some is None:
         raise TypeError("expected d_h, or d_z and h")
@@ -304,7 +305,7 @@ def join_grad(d_h, d_z, h, y=None, after=None, gate=None, scale: float = 1.0, dr
         if g_h is not None:
             _fits(g_h, "out.h", shape, (dtype,), device)
         if g_y is not None:
-            _fits(g_y, "out.y", shape, (y.dtype,) if y is not None else (), device)
+            _fits(g_y, "out.y", shape, _FLOAT if y is None else (y.dtype,), device)
         if g_after is not None:
             _fits(g_after, "out.after", (H,), _F32, device)
         if g_gate is not None:
@@ -317,9 +318,10 @@ def join_grad(d_h, d_z, h, y=None, after=None, gate=None, scale: float = 1.0, dr
     if scratch is not None:
         _fits(scratch, "scratch", scratch.shape, _U8, device)
         room = scratch.numel()
+    like_y = y if y is not None else g_y
     r = L.moe_join_grad(_ptr(d_h), _ptr(d_z), None if d_z is None else h.data_ptr(), _ptr(y), _ptr(after), _ptr(gate),
                         _ptr(before), seeds, _ptr(g_h), _ptr(g_y), _ptr(g_after), _ptr(g_gate), _ptr(g_before),
-                        T, H, _TYPES[dtype], 0 if y is None else _TYPES[y.dtype], 0 if d_z is None else _TYPES[d_z.dtype],
+                        T, H, _TYPES[dtype], 0 if like_y is None else _TYPES[like_y.dtype], 0 if d_z is None else _TYPES[d_z.dtype],
                         w_type, kind, scale, drop, eps, scratch.data_ptr() if room else None, room, handle)
     if r < 0:
         raise MoeError(r, "moe_join_grad")

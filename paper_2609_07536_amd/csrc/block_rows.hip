@@ -1064,12 +1064,14 @@ extern "C" int moe_join_grad(const void* dx, const void* dz, const void* x, cons
                              int32_t y_type, int32_t z_type, int32_t w_type, int32_t gate_kind, float scale,
                              double drop, float eps, void* scratch, size_t scratch_bytes, void* stream) {
   JoinArgs a = {};
-  a.dx = dx, a.dz = dz, a.h = x, a.y = y, a.after = after, a.gate = gate, a.before = before, a.rng = rng;
+  const bool reads_y = after || gate_kind != MOE_GATE_NONE;
+  a.dx = dx, a.dz = dz, a.h = x, a.after = after, a.gate = gate, a.before = before, a.rng = rng;
   a.dh = dh, a.dy = dy, a.d_after = d_after, a.d_gate = d_gate, a.d_before = d_before;
+  a.y = y || reads_y ? y : dy;   // (that there was one is all that matters)
   const int bad = check_join(a, T, H, h_type, y_type, z_type, w_type, gate_kind, drop);
   if (bad) return bad;
   if ((d_after && !after) || (d_before && !before) || (d_gate && gate_kind == MOE_GATE_NONE)) return MOE_ERR_INVALID_ARG;
-  if (T > 0 && ((!dx && !dz) || (dz && (!before || !x)) || (dy && !y))) return MOE_ERR_INVALID_ARG;
+  if (T > 0 && ((!dx && !dz) || (dz && (!before || !x)) || (dy && !a.y))) return MOE_ERR_INVALID_ARG;
   const void* outs[5] = {dh, dy, d_after, d_gate, d_before};
   for (const void* o : outs)
     for (const void* in : {dz, x, y, after, gate, before, (const void*)rng})
@@ -1094,11 +1096,10 @@ extern "C" int moe_join_grad(const void* dx, const void* dz, const void* x, cons
   auto launch = [&](const JoinArgs& a) {
     with_grad_row(H, [&](auto shape) {
       constexpr int NT = decltype(shape)::lanes, U = decltype(shape)::each;
-      const bool use_y = a.after || a.gate_kind != MOE_GATE_NONE;
       const int threads = threads_of(shape, H, 4);
 #define MOE_GRAD(H16, Y16, Z16)                                                      \
-  use_y ? join_grad_kernel<NT, U, H16, Y16, Z16, true><<<(unsigned)G, threads, 0, s>>>(a) \
-        : join_grad_kernel<NT, U, H16, Y16, Z16, false><<<(unsigned)G, threads, 0, s>>>(a)
+  reads_y ? join_grad_kernel<NT, U, H16, Y16, Z16, true><<<(unsigned)G, threads, 0, s>>>(a) \
+          : join_grad_kernel<NT, U, H16, Y16, Z16, false><<<(unsigned)G, threads, 0, s>>>(a)
       switch (4 * a.h16 + 2 * a.y16 + a.z16) {
         case 0: MOE_GRAD(false, false, false); break;
         case 1: MOE_GRAD(false, false, true); break;

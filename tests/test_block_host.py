@@ -257,3 +257,16 @@ def test_a_differentiable_join_with_dropout_refuses_to_go_without_numbers():
         A.join(x, x, drop=0.5)
     with pytest.raises(TypeError):
         K.join(x, x, drop=0.5)
+
+
+def test_join_grad_without_y_where_it_is_not_read():
+    """With neither a norm after the block nor a gate dy says that the join had y.  (The calls
+    that are taken get as far as their missing scratch.)"""
+    plain = dict(y=None, after=None, gate=None, kind=0, d_after=None, d_gate=None, scratch=None)
+    assert _grad(**plain) == B.MOE_ERR_WORKSPACE
+    assert _grad(**plain, **{"drop": 0.0}) == B.MOE_ERR_WORKSPACE
+    assert _grad(**{**plain, "dy": None}) == B.MOE_ERR_INVALID_ARG                 # dropout of nothing
+    assert _grad(**{**plain, "after": 5 * P}) == B.MOE_ERR_INVALID_ARG
+    assert _grad(**{**plain, "gate": 6 * P, "kind": 2}) == B.MOE_ERR_INVALID_ARG
+    assert _grad(**{**plain, "gate": 6 * P, "kind": 1, "drop": 0.0}) == B.MOE_ERR_INVALID_ARG
+    assert _grad(**{**plain, "dy": 10 * P + 1}) == B.MOE_ERR_ALIGNMENT

@@ -348,3 +348,29 @@ def test_differentiable_join_by_what_is_used(gpu_lib, used, kind):
             continue
         off = (a[k].grad.double() - want).abs().max() / want.abs().max()
         assert off <= 1e-4, (k, float(off))
+
+
+@pytest.mark.parametrize("y_type", ["bfloat16", "float32"])
+def test_backward_of_a_join_takes_no_memory_beside_its_gradients(gpu_lib, y_type):
+    """y is not read again without a norm after the block and a gate: the backward pass has
+    room for the gradients of h and y and, but for 1 MiB, for nothing else."""
+    import torch
+
+    from paper_2609_07536_amd import autograd as A
+    T, H = 4096, 1024
+    h = torch.randn(T, H, device="cuda").requires_grad_()
+    y = torch.randn(T, H, device="cuda").to(getattr(torch, y_type)).requires_grad_()
+    x, z = A.join(h, y, scale=0.5, before=torch.ones(H, device="cuda"))
+    dx, dz = torch.randn_like(x), torch.randn_like(z)
+    want = h.numel() * h.element_size() + y.numel() * y.element_size()
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    base = torch.cuda.memory_allocated()
+    gh, gy = torch.autograd.grad((x, z), (h, y), (dx, dz))
+    assert torch.cuda.max_memory_allocated() - base <= want + 2 ** 20
+    assert torch.equal(gy, (0.5 * gh).to(y.dtype))
+    # a block's output without a gradient, dropout and all
+    rng = torch.tensor([1, 2], device="cuda")
+    x, z = A.join(h, y.detach(), scale=0.5, drop=0.25, rng=rng, before=torch.ones(H, device="cuda"))
+    g, = torch.autograd.grad(x, h, dx)
+    assert torch.equal(g, dx)
