@@ -116,7 +116,8 @@ int moe_join_grad(const void* dx, const void* dz, const void* x, const void* y, 
  * not matter, before or after. */
 size_t moe_few_scratch_size(int32_t T, int32_t H, int32_t I, int32_t E, int32_t topk);
 
-/* The layer in two launches, without a sort, each hit expert's weights read once.
+/* The layer in two launches, without a sort, each hit expert's weights read once (in mx4, of
+ * more than eight tokens, w1 once for every seven that name the expert).
  *   hidden      device bf16 [T, H] (16-byte aligned)
  *   w1, w2      as moe_layer_forward takes them: [E, H, 2 I] packed by
  *               moe_gemm1_pack_weights and [E, I, H], 16-byte aligned

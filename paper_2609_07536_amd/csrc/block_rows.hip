@@ -84,10 +84,10 @@ __device__ __forceinline__ int ordered(float v) {
 }
 
 // Bound by the instructions of the rounds: for each logit of a lane two comparisons and two
-// selections (16384 tokens, 8 of 256 experts by sixteen lanes a token: 10.8 us, of which
-// the launch and 18 MB are some 5; by eight lanes 11.2; a threshold found bit by bit over a
-// wave's counts 15).  The chosen go through LDS to the lanes that take their scores: slot
-// j is lane j % L's.
+// selections (16384 tokens, 8 of 256 experts by sixteen lanes a token: a call takes 10.8 us,
+// of which the launch and 18 MB are some 5, and 9.3 of bf16 logits; by eight lanes 11.2; a
+// threshold found bit by bit over a wave's counts 15).  The chosen go through LDS to the lanes
+// that take their scores: slot j is lane j % L's.
 template <class T, int L, int R>
 __global__ void __launch_bounds__(256) choose_kernel(const T* logits, const float* bias, int32_t* ids, float* gates,
                                                      long long first, int tokens, int E, int topk, bool softmax,
@@ -176,8 +176,9 @@ __global__ void __launch_bounds__(256) choose_kernel(const T* logits, const floa
 //   sigmoid                s p_e (1 - p_e) g
 // An expert that several slots name enters by its number of slots `cnt` and their sum.
 // A token's logits, and in the end its gradients, stay in the registers of its lanes.  Bound by
-// latency at training's sizes (8192 tokens, 4 of 30 experts: 5.2 us for 2.2 MB, half of it the
-// launch).
+// latency at training's sizes (8192 tokens, 4 of 30 experts: 5.3 us for 2.2 MB, and the same for
+// 1.2 MB in bf16, half of it the launch): the flag of a bad id stands between a slot's loads and
+// the next one's, so that the slots' are waited for one after the other.
 template <class T, int L, int R>
 __global__ void __launch_bounds__(256) choose_grad_kernel(const float* dgates, const T* logits, const int32_t* ids,
                                                           T* dlogits, long long first, int tokens, int E, int topk, bool softmax,
@@ -439,8 +440,10 @@ __device__ __forceinline__ void row_sums(float (&v)[n], float* lds) {
 
 // A workgroup takes a row, U chunks of eight columns a thread, all of it in registers:
 // every tensor is read and written once.  Bound by memory: 16384 rows of 2048, h, x and z in
-// bf16 and y in fp32, 59.4 us for 336 MB (5.6 TB/s; a large copy 4.9).  A few rows by latency: one
-// 2.6 us; 777 of 1352 with the norm after the block, a gate of tokens and dropout 5.9.
+// bf16 and y in fp32, 60 us for 336 MB (5.6 TB/s; a large copy 4.9); 4096 rows of 4096, 2048 of 8192
+// and 1024 of 16384, all in bf16, 29, 34 and 33 us for 134 MB.  A few rows by latency: one 2.6 us;
+// 777 of 1352 with the norm after the block, a gate of tokens and dropout 5.9: the weights' loads
+// and the random numbers, which wait for no sum, stand behind the sums all the same.
 template <int NT, int U>
 __global__ void __launch_bounds__(NT) join_kernel(JoinArgs a, long long first) {
   __shared__ float lds[NT / 64];
@@ -525,14 +528,19 @@ __global__ void __launch_bounds__(NT) join_kernel(JoinArgs a, long long first) {
 // The gradient: with v = dz before, r the norm's factor and D = dx + r (v - x r^2
 // mean(x v)), dh = D, da = scale drop(D), db = gate da, and dy is db or, by the same
 // formula, its way back through the norm after the block.  Workgroup g takes rows g,
-// g + G, ..., the next one's loads under way while it works on one, four columns a thread (so
-// that what a thread keeps fits its registers); its sums over rows of the columns'
-// gradients go to `parts` [array][G][H] and are added up by a second launch, always in the
-// same order.  Rows of up to 4096 columns keep these sums, and the weights, in registers;
-// longer ones (kLong) keep the sums in LDS and load weights and columns again.  Bound by memory:
-// 8192 rows of 2048 in bf16 with the norm before, 33.0 us and 4.6 for the second launch, 201 MB
-// (5.5 TB/s); 777 rows of 1351 in fp32 with everything, 14.2 and 4.1 for 23 MB: two rows a
-// workgroup, whose two sums over the row and random numbers stand one after the other.
+// g + G, ..., four columns a thread (so that what a thread keeps fits its registers); its sums
+// over rows of the columns' gradients go to `parts` [array][G][H] and are added up by a second
+// launch, always in the same order.  Rows of up to 4096 columns keep these sums, and the weights,
+// in registers, and ask for the next row before they work on one.  That row is under way
+// meanwhile where all that is read is bf16; an fp32 tensor's settle() may leave loads of its own
+// for the first sum over the row (rows of fewer than four columns), a bf16 gate of tokens is
+// converted where it is loaded, and with either the compiler waits for all loads there.  Longer
+// rows (kLong) keep the sums in LDS and load weights and columns again.  Bound by memory: 8192
+// rows of 2048 in bf16 with the norm before, 33.0 us and 4.6 for the second launch, 168 MB (5.1 TB/s);
+// with an fp32 stream and y 57.1 and 4.7, 302 MB (5.3).  4096 rows of 4096 in bf16 36.0 and 4.6 for the
+// same 168 MB, but 2048 of 8192, whose columns come twice, 68.8 and 4.8.  777 rows of 1351 in fp32 with
+// everything, 14.5 and 4.2 for 23 MB, by latency: two rows a workgroup, each waited for, with two
+// sums over the row and the random numbers one after the other.
 // Types are the kernel's own (B16: bf16, else fp32), so that a row is as few registers as it
 // is bytes; kY: with a norm after the block or a gate (else y is not read).
 template <bool B16>

@@ -2,7 +2,8 @@
 //
 // A token's row is a row of the 16x16x32 matrix instruction, so one instruction
 // takes all tokens through 32 of K and 16 columns of an expert's weights.  Weights go
-// straight from memory to registers, each read once, with no stop in LDS: what bounds the
+// straight from memory to registers, each read once (but 4-bit ones of the first launch once for
+// seven tokens, where there are more than eight), with no stop in LDS: what bounds the
 // layer is their stream, and the first launch's loads need nothing but the choice itself.
 #include <hip/hip_runtime.h>
 
@@ -214,9 +215,9 @@ __device__ __forceinline__ u32x4 row_operand(const uint8_t* lds, int row, int j,
 
 // ---- the first launch ------------------------------------------------------------------
 
-// A workgroup's expert and the tokens that name it (bit t); false: nothing to do.  Lane t
-// looks through token t's slots; the loads of eight are under way together, and wait for
-// nothing.
+// A workgroup's expert and the tokens that name it (bit t); false: nothing to do.  The
+// workgroup's own slot comes first, by itself; then lane t looks through token t's slots, eight
+// at a time, whose loads (the eighth's in a branch) are under way together.
 __device__ __forceinline__ bool few_unit(const FewArgs& a, int u, int* e, uint32_t* tokens) {
   const int t = threadIdx.x & 63;
   const bool by_slot = a.slots <= a.E;
@@ -298,8 +299,8 @@ __device__ __forceinline__ void put_act(const FewArgs& a, int unit, int t, int o
 
 // 64 packed columns (32 outputs), the waves taking every W-th 32 of K.  Bound by the stream of
 // the weights: 16 tokens, 32 experts of 2048 x 704, 34 us for 185 MB (5.4 TB/s); one token, 6
-// experts, 9.3 us for 35 MB, a quarter of it the launch (sixteen waves a workgroup, for twice
-// the loads under way: 9.3 too).
+// experts, 9 to 10 us for 35 MB, a quarter of it the launch (sixteen waves a workgroup, for twice
+// the loads under way: equal).
 constexpr int kCols = 64;
 template <int W>
 __global__ void __launch_bounds__(64 * W) few_up_kernel(FewArgs a) {
@@ -344,7 +345,9 @@ __global__ void __launch_bounds__(64 * W) few_up_kernel(FewArgs a) {
 // layer of 9 and 16 tokens 15.2 and 16.5 us so, 12.1 and 13.2 now; 32 of 2048 x 704 27.2 and 29.6,
 // 26.2 and 29.1; 1024 x 512, top 8, 16 tokens 17.2 and 17.8; all passes on registers in one loop
 // 30 and more).  One token, 6 experts of 2048 x 704: 7.3 us for 9 MB, one step a wave, that is
-// the launch and a chain of the choice, the loads and the sum over waves; 8 tokens, 24 experts:
+// the launch and a chain of loads, each waited for before the next: the own slot, the tokens' slots,
+// the tokens' rows, and the codes and scales, which the two ways to load scales (load()) keep apart;
+// then the sum over waves.  8 tokens, 24 experts:
 // some 15 us for 37 MB.
 template <int R, int W, bool kMany, bool kOdd>
 __global__ void __launch_bounds__(64 * W) few_up_mx4_kernel(FewArgs a) {
@@ -613,7 +616,8 @@ __global__ void __launch_bounds__(64 * W) few_down_kernel(FewArgs a) {
 // to 15 the other: the tokens that name the expert, one after the other, so that more than R
 // of them, which take another pass over the codes that are there, are rare.  16 tokens, 32
 // experts of 2048 x 704: 13.7 us for 25 MB, one token 5.6 us: bound by latency, one to four steps
-// a wave between the list and the join (the next step's codes under way while a step is worked
+// a wave between the list and the join, each waiting for its codes and scales before it asks for the
+// tokens' rows (the next step's codes under way while a step is worked
 // on: equal, the other waves hide it).
 template <int R, int W, int kPasses>
 __global__ void __launch_bounds__(64 * W) few_down_mx4_kernel(FewArgs a) {
